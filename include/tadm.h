@@ -168,6 +168,116 @@ int32_t tadm_context_length(const tadm_context* ctx);
 tadm_status tadm_context_reset(tadm_context* ctx);
 tadm_status tadm_context_destroy(tadm_context* ctx);
 
+/* ----------------------------------------------------- paged 8-bit K/V ---- */
+/* A set of pages.  A page holds TADM_PAGE positions of every layer in 8 bits: per layer and
+ * K/V head the keys [TADM_PAGE, head_dim], then the values transposed
+ * [head_dim, TADM_PAGE], as e4m3 codes, and a float32 scale for each of the two.  A code c
+ * stands for c * scale.  Scales are powers of two, so that the value of a code is exact in
+ * bf16 and float32.
+ *   data   [n_pages, n_layers, n_kv_heads, 2, TADM_PAGE * head_dim]  (16-byte aligned)
+ *   scale  [n_pages, n_layers, n_kv_heads, 2]
+ * A program may own its pages (the operators below take any such arrays) or have a
+ * tadm_pool manage them.  n_kv_heads and head_dim are the model's. */
+enum { TADM_PAGE = 64 };
+typedef struct {
+  void* data;
+  float* scale;
+  int32_t n_pages, n_layers, n_kv_heads, head_dim;
+} tadm_pages;
+
+/* The batch of a call.  Row b's positions [TADM_PAGE i, TADM_PAGE (i + 1)) are on page
+ * table_dev[b * max_pages + i]; an id outside [0, n_pages) is an absent page: nothing is
+ * written to it, and its positions take no part in attention.  The row holds
+ * positions [0, len_b): len_b = len for every row, or with len_dev len_dev[b] cut to
+ * [0, len].  Its window has n_b new tokens: n, or n_dev[b] cut to [0, n] (n is an
+ * argument of each call).  Lengths on the device are not read on the host, so a captured
+ * call serves any lengths within len and n. */
+typedef struct {
+  const int32_t* table_dev; /* int32 [B, max_pages] */
+  const int32_t* len_dev;   /* nullable int32 [B] */
+  const int32_t* n_dev;     /* nullable int32 [B] */
+  int32_t B, max_pages;
+  int32_t len;              /* <= max_pages * TADM_PAGE */
+} tadm_page_rows;
+
+/* Quantises a window into the rows' pages of one layer: keys k_dev [B, Hkv, cap, head_dim] and
+ * transposed values vt_dev [B, Hkv, head_dim, cap] of the model dtype (the layouts of
+ * tadm_context_read; cap a multiple of 64, 16-byte aligned) go to positions
+ * [len_b, len_b + n_b); tokens past the table are dropped (TADM_ERR_INVALID when
+ * len + n of a call without len_dev says so).  Per page, head and side, with M the
+ * largest finite magnitude of the new values: e = the least exponent with M <= 448 2^e,
+ * in [-110, 120]; where the page holds earlier positions of the row the scale becomes
+ * the larger of the present one and 2^e, and their codes are rounded again if it grew.
+ * code(x) = x / scale rounded to nearest even; infinities and NaN become the NaN code.
+ * Codes of other positions stay as they are, and so do the rows' lengths (the caller
+ * advances them).  No two rows may write the same page. */
+tadm_status tadm_pages_append(tadm_model* m, const tadm_pages* p, int32_t layer, const tadm_page_rows* rows,
+                              const void* k_dev, const void* vt_dev, int32_t n, int32_t cap);
+/* Attention of a window over the rows' pages of one layer: for every query q_dev
+ * [B, n_heads, n, head_dim] of the n_b first of a row,
+ *   o = softmax(q k^T / sqrt(head_dim)) v
+ * over the positions [0, len_b) on present pages and, unless k_dev and vt_dev are NULL,
+ * over the window's own n_b tokens (arrays as in append; every query sees every one of them).
+ * Query head h reads K/V head floor(h n_kv_heads / n_heads).  o_dev [B, n, n_heads *
+ * head_dim] has the model dtype, lse_dev [B, n_heads, n] (float32, nullable) receives the
+ * logarithm of the softmax's denominator; a query without a key gets 0 and -inf, and rows
+ * at and behind n_b keep what they had.  A position with a NaN code makes the rows that
+ * see it NaN.  q_dev, k_dev, vt_dev and o_dev are 16-byte aligned.  work_dev
+ * (16-byte aligned, nullable when the size is 0) is scratch of at least
+ * tadm_pages_attend_work bytes: calls that may overlap, captured ones among them, need
+ * scratch of their own; it needs no clearing. */
+tadm_status tadm_pages_attend(tadm_model* m, const tadm_pages* p, int32_t layer, const tadm_page_rows* rows,
+                              const void* q_dev, int32_t n, const void* k_dev, const void* vt_dev, int32_t cap,
+                              void* o_dev, float* lse_dev, void* work_dev, size_t work_bytes);
+/* Scratch of a tadm_pages_attend call with these rows (B and len) and n; 0 for invalid arguments. */
+size_t tadm_pages_attend_work(const tadm_model* m, const tadm_page_rows* rows, int32_t n);
+/* The positions [0, len_b) of one layer as keys k_dev [B, Hkv, cap, head_dim] and transposed
+ * values vt_dev [B, Hkv, head_dim, cap] of the model dtype, exactly; zeros for absent
+ * pages, other columns stay as they are.  cap >= len, a multiple of 64. */
+tadm_status tadm_pages_read(tadm_model* m, const tadm_pages* p, int32_t layer, const tadm_page_rows* rows,
+                            void* k_dev, void* vt_dev, int32_t cap);
+/* Page dst[i] <- page src[i] in every layer, codes and scales, for i < n_copies.  src and dst are
+ * host arrays, read before the call returns.  A page may be copied to several places; no
+ * destination may appear twice or be a source as well. */
+tadm_status tadm_pages_copy(tadm_model* m, const tadm_pages* p, const int32_t* src, const int32_t* dst,
+                            int32_t n_copies);
+
+/* A pool: pages of a model with reference counts, from which contexts take what they need.
+ * tadm_pool_create allocates n_pages pages on the model's device (n_pages x n_layers x
+ * n_kv_heads x 128 x head_dim bytes).  A pool outlives its contexts (TADM_ERR_STATE
+ * otherwise) and is destroyed before its model. */
+typedef struct tadm_pool tadm_pool;
+tadm_status tadm_pool_create(tadm_model* m, int32_t n_pages, tadm_pool** out);
+tadm_status tadm_pool_destroy(tadm_pool* pool);
+/* Pages in all, and pages that no context holds (0 for NULL). */
+int32_t tadm_pool_size(const tadm_pool* pool);
+int32_t tadm_pool_free_pages(const tadm_pool* pool);
+/* The pool's arrays for the operators above; valid until tadm_pool_resize. */
+tadm_status tadm_pool_pages(const tadm_pool* pool, tadm_pages* out);
+/* Moves the held pages to the lowest ids, in the contexts' tables too (enqueued like any work). */
+tadm_status tadm_pool_compact(tadm_pool* pool);
+/* Compacts, then gives the pool n_pages pages (at least those held, TADM_ERR_INVALID otherwise) in a
+ * new allocation.  Waits for the device; captured work on the pool is void. */
+tadm_status tadm_pool_resize(tadm_pool* pool, int32_t n_pages);
+
+/* A context (see above) whose K, V are pages of a pool: every call that takes a context
+ * takes it.  Committed positions are held in 8 bits; the active window's K, V stay in
+ * the model dtype.  Pages are taken as positions are appended: tadm_context_append
+ * returns TADM_ERR_OOM, without side effects, when the pool has too few.  reset and
+ * destroy give them back.  tadm_context_read returns the pages' values. */
+tadm_status tadm_context_create_pooled(tadm_model* m, tadm_pool* pool, int32_t B, int32_t max_ctx,
+                                       tadm_context** out);
+/* A new context of B rows with the length and capacity of `src`, row b holding what row rows[b] (host
+ * array; a row may be taken several times) of src holds.  The pages are shared until one
+ * of their holders appends to a page that others hold too, which first copies that page.
+ * src must be a pooled context (TADM_ERR_STATE otherwise). */
+tadm_status tadm_context_fork(const tadm_context* src, const int32_t* rows, int32_t B, tadm_context** out);
+/* Drops the positions [len, tadm_context_length) of any context; a pooled one gives back the
+ * pages that hold none of the others. */
+tadm_status tadm_context_truncate(tadm_context* ctx, int32_t len);
+/* The rows of a pooled context for the operators above (valid until it is destroyed; len as of now). */
+tadm_status tadm_context_rows(const tadm_context* ctx, tadm_page_rows* out);
+
 /* ------------------------------------------------------------ the step ---- */
 /* Anchor refresh (Alg. 1): c = S(canvas), h = A(c), written to `cache`.
  * canvas_dev [B, L] is the window at positions [ctx_len, ctx_len + L) (ctx may be

@@ -18,10 +18,12 @@ computes, written from the paper:
   and the self-conditioning signal;
 * ``train``    -- the pretraining objective (Theorem T-ANELBO with gamma = 0, sigma = 0):
   training times with stale anchors, the corrupted pair (z_t, z_t') and the
-  1/t-weighted masked cross-entropy.
+  1/t-weighted masked cross-entropy;
+* ``pages``    -- the paged 8-bit K/V store: e4m3 quantisation with power-of-two scales,
+  append, read and attention.
 
 Only ``tests/``, ``__graft_entry__.smoke()`` and the benchmark's ``cpu_baseline``
 leg may import this package.  It shares no code with the GPU path; the only common
 dependency is the seeded input module ``synth``.
 """
-from . import network, sampler, loop, usdm, train  # noqa: F401
+from . import network, sampler, loop, usdm, train, pages  # noqa: F401

@@ -55,6 +55,16 @@ STEP_RANKED, STEP_REMASK, STEP_ENTROPY = 0, 1, 2
 SAMPLER_LOOP, SAMPLER_ENTROPY = 2, 3
 
 
+class tadm_pages(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("scale", C.c_void_p), ("n_pages", C.c_int32), ("n_layers", C.c_int32),
+                ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32)]
+
+
+class tadm_page_rows(C.Structure):
+    _fields_ = [("table_dev", C.c_void_p), ("len_dev", C.c_void_p), ("n_dev", C.c_void_p), ("B", C.c_int32),
+                ("max_pages", C.c_int32), ("len", C.c_int32)]
+
+
 class TadmError(RuntimeError):
     def __init__(self, status, msg):
         super().__init__(f"tadm status {status}: {msg}")
@@ -81,6 +91,22 @@ _SIGS = {
     "tadm_context_destroy": (_I, [_P]),
     "tadm_anchor_forward": (_I, [_P, _P, _P, _I, _I, _I, _I, _P]),
     "tadm_anchor_forward_sc": (_I, [_P, _P, _P, _I, _I, _I, _I, _P, _I, _P]),
+    "tadm_pages_append": (_I, [_P, _P, _I, _P, _P, _P, _I, _I]),
+    "tadm_pages_attend": (_I, [_P, _P, _I, _P, _P, _I, _P, _P, _I, _P, _P, _P, C.c_size_t]),
+    "tadm_pages_attend_work": (C.c_size_t, [_P, _P, _I]),
+    "tadm_pages_read": (_I, [_P, _P, _I, _P, _P, _P, _I]),
+    "tadm_pages_copy": (_I, [_P, _P, _P, _P, _I]),
+    "tadm_pool_create": (_I, [_P, _I, C.POINTER(_P)]),
+    "tadm_pool_destroy": (_I, [_P]),
+    "tadm_pool_size": (_I, [_P]),
+    "tadm_pool_free_pages": (_I, [_P]),
+    "tadm_pool_pages": (_I, [_P, C.POINTER(tadm_pages)]),
+    "tadm_pool_compact": (_I, [_P]),
+    "tadm_pool_resize": (_I, [_P, _I]),
+    "tadm_context_create_pooled": (_I, [_P, _P, _I, _I, C.POINTER(_P)]),
+    "tadm_context_fork": (_I, [_P, _P, _I, C.POINTER(_P)]),
+    "tadm_context_truncate": (_I, [_P, _I]),
+    "tadm_context_rows": (_I, [_P, C.POINTER(tadm_page_rows)]),
     "tadm_entropy_inv_temp": (C.c_float, [_I, _I, C.c_float, C.c_float]),
     "tadm_train_loss": (_I, [_P, _P, _I, _I, _P, _P, C.c_float, C.c_uint64, C.c_uint32, _P, _P, _P, _P]),
     "tadm_stale_times": (None, [_I, C.c_uint64, C.c_uint32, C.c_float, _P, _P, _P, _P, _P]),
@@ -110,6 +136,7 @@ for _name, (_res, _args) in _SIGS.items():
 
 EXPORTED = sorted(_SIGS)
 NOALLOC_MAX_POSITIONS = 65536  # TADM_NOALLOC_MAX_POSITIONS
+PAGE = 64  # TADM_PAGE: positions of a page
 
 
 def last_error():
@@ -211,6 +238,113 @@ def tadm_context_reset(ctx):
 
 def tadm_context_destroy(ctx):
     check(lib.tadm_context_destroy(ctx))
+
+
+# ------------------------------------------------------- paged 8-bit K/V
+def page_set(data, scale):
+    """Descriptor of pages in the caller's tensors: data uint8 (or float8_e4m3fn)
+    [n_pages, n_layers, Hkv, 2, 64 * head_dim], scale float32 [n_pages, n_layers, Hkv, 2],
+    both contiguous and kept alive by the caller."""
+    n_pages, n_layers, heads, two, width = data.shape
+    if two != 2 or width % PAGE or tuple(scale.shape) != (n_pages, n_layers, heads, 2):
+        raise ValueError(f"pages of shape {tuple(data.shape)} with scales of shape {tuple(scale.shape)}")
+    if data.element_size() != 1 or scale.element_size() != 4:
+        raise ValueError("pages hold 8-bit codes and float32 scales")
+    if not (data.is_contiguous() and scale.is_contiguous()):
+        raise ValueError("pages and scales must be contiguous")
+    return tadm_pages(data=ptr(data), scale=ptr(scale), n_pages=n_pages, n_layers=n_layers, n_kv_heads=heads,
+                      head_dim=width // PAGE)
+
+
+def page_rows(table, length, len_dev=None, n_dev=None):
+    """Descriptor of a batch: table int32 [B, max_pages] on the device, length the committed
+    positions of every row, or the most of any row when the device tensor len_dev (int32
+    [B]) has each row's; n_dev (int32 [B]) the tokens of each row's window.  The caller
+    keeps the tensors alive."""
+    return tadm_page_rows(table_dev=ptr(table), len_dev=ptr(len_dev), n_dev=ptr(n_dev), B=table.shape[0],
+                          max_pages=table.shape[1], len=length)
+
+
+def tadm_pages_append(m, pages, layer, rows, k, vt, n, cap):
+    check(lib.tadm_pages_append(m, C.byref(pages), layer, C.byref(rows), ptr(k), ptr(vt), n, cap))
+
+
+def tadm_pages_attend(m, pages, layer, rows, q, n, k, vt, cap, o, lse, work):
+    """work: a device tensor of at least tadm_pages_attend_work bytes (None when that is 0)."""
+    check(lib.tadm_pages_attend(m, C.byref(pages), layer, C.byref(rows), ptr(q), n, ptr(k), ptr(vt), cap, ptr(o),
+                                ptr(lse), ptr(work), 0 if work is None else work.numel() * work.element_size()))
+
+
+def tadm_pages_attend_work(m, rows, n):
+    return lib.tadm_pages_attend_work(m, C.byref(rows), n)
+
+
+def tadm_pages_read(m, pages, layer, rows, k, vt, cap):
+    check(lib.tadm_pages_read(m, C.byref(pages), layer, C.byref(rows), ptr(k), ptr(vt), cap))
+
+
+def tadm_pages_copy(m, pages, src, dst):
+    """src, dst: equally long sequences (or int32 arrays) of page ids on the host."""
+    import numpy as np
+    src, dst = (np.ascontiguousarray(a, dtype=np.int32) for a in (src, dst))
+    if src.shape != dst.shape or src.ndim != 1:
+        raise ValueError(f"{src.shape} sources for {dst.shape} destinations")
+    check(lib.tadm_pages_copy(m, C.byref(pages), src.ctypes.data, dst.ctypes.data, len(src)))
+
+
+def tadm_pool_create(m, n_pages):
+    p = C.c_void_p()
+    check(lib.tadm_pool_create(m, n_pages, C.byref(p)))
+    return p
+
+
+def tadm_pool_destroy(pool):
+    check(lib.tadm_pool_destroy(pool))
+
+
+def tadm_pool_size(pool):
+    return lib.tadm_pool_size(pool)
+
+
+def tadm_pool_free_pages(pool):
+    return lib.tadm_pool_free_pages(pool)
+
+
+def tadm_pool_pages(pool):
+    p = tadm_pages()
+    check(lib.tadm_pool_pages(pool, C.byref(p)))
+    return p
+
+
+def tadm_pool_compact(pool):
+    check(lib.tadm_pool_compact(pool))
+
+
+def tadm_pool_resize(pool, n_pages):
+    check(lib.tadm_pool_resize(pool, n_pages))
+
+
+def tadm_context_create_pooled(m, pool, B, max_ctx):
+    c = C.c_void_p()
+    check(lib.tadm_context_create_pooled(m, pool, B, max_ctx, C.byref(c)))
+    return c
+
+
+def tadm_context_fork(src, rows):
+    """rows: the row of src that each row of the new context starts from."""
+    c = C.c_void_p()
+    check(lib.tadm_context_fork(src, (C.c_int32 * len(rows))(*rows), len(rows), C.byref(c)))
+    return c
+
+
+def tadm_context_truncate(ctx, length):
+    check(lib.tadm_context_truncate(ctx, length))
+
+
+def tadm_context_rows(ctx):
+    r = tadm_page_rows()
+    check(lib.tadm_context_rows(ctx, C.byref(r)))
+    return r
 
 
 def tadm_anchor_forward(m, ctx, canvas, B, L, i, T, cache):

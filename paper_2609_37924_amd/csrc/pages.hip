@@ -1,0 +1,202 @@
+// Append, read and copy of the paged 8-bit K/V store.
+//
+// Quantisation of one page, head and side: with M the largest finite |x| among the new values,
+// e = the least exponent with M <= 448 2^e (448 is the largest e4m3), cut to [-110, 120]; a
+// page that holds earlier positions of the row keeps the larger of its scale and 2^e, and if
+// it grew its codes are rounded again to the new scale.  code(x) = x 2^-e rounded to nearest
+// even; values that are not finite get the NaN code.  A power of two costs no precision: the
+// codes are floating point, and 2^-e x is exact.
+#include "common.h"
+#include "pages.h"
+
+namespace tadm {
+namespace {
+
+__device__ __forceinline__ int row_len(const PageRows& r, int b) {
+  return r.len ? min(max(r.len[b], 0), r.max_len) : r.max_len;
+}
+__device__ __forceinline__ int row_new(const PageRows& r, int b) {
+  return r.n ? min(max(r.n[b], 0), r.max_n) : r.max_n;
+}
+
+// 2^e of the least e in [PAGE_E_MIN, PAGE_E_MAX] with top <= 448 2^e = 1.75 2^(e + 8)
+__device__ __forceinline__ float scale_of(float top) {
+  const uint32_t bits = __float_as_uint(top);
+  int e = (int)(bits >> 23) - 127 - 8 + ((bits & 0x7fffffu) > 0x600000u ? 1 : 0);
+  e = min(max(e, PAGE_E_MIN), PAGE_E_MAX);
+  return __uint_as_float((uint32_t)(e + 127) << 23);
+}
+__device__ __forceinline__ float finite_abs(float x) {
+  const float a = fabsf(x);
+  return a < INFINITY ? a : 0.f;
+}
+__device__ __forceinline__ uint8_t code_of(float x, float inv) {
+  const int c = __builtin_amdgcn_cvt_pk_fp8_f32(x * inv, 0.f, 0, false) & 255;
+  return fabsf(x) < INFINITY ? c : 0x7f;
+}
+__device__ __forceinline__ float value_of(uint8_t c) { return __builtin_amdgcn_cvt_f32_fp8((int)c, 0); }
+
+// One block per (page of a row, K/V head, row).
+template <class T>
+__global__ __launch_bounds__(256) void append_kernel(PageLayer p, PageRows r, const T* k, const T* vt, int cap) {
+  __shared__ float red[2][4];
+  const int b = blockIdx.z, h = blockIdx.y, dh = p.dh;
+  const int len = row_len(r, b);
+  const int slot = len / PAGE + blockIdx.x, start = slot * PAGE;
+  if (slot >= r.max_pages) return;
+  const int lo = max(len, start), hi = min(len + row_new(r, b), start + PAGE);
+  if (hi <= lo) return;
+  const int page = r.table[(size_t)b * r.max_pages + slot];
+  if ((unsigned)page >= (unsigned)p.n_pages) return;
+  const int m = hi - lo;
+  const T* ks = k + (((size_t)b * p.Hkv + h) * cap + (lo - len)) * dh;  // m rows of dh
+  const T* vs = vt + ((size_t)b * p.Hkv + h) * dh * cap + (lo - len);   // dh rows of m
+  float tk = 0.f, tv = 0.f;
+  for (int i = threadIdx.x; i < m * dh; i += 256) {
+    tk = fmaxf(tk, finite_abs(f32_of(ks[i])));
+    tv = fmaxf(tv, finite_abs(f32_of(vs[(size_t)(i / m) * cap + i % m])));
+  }
+  tk = wave_max(tk);
+  tv = wave_max(tv);
+  if (threadIdx.x % 64 == 0) {
+    red[0][threadIdx.x / 64] = tk;
+    red[1][threadIdx.x / 64] = tv;
+  }
+  __syncthreads();
+  uint8_t* codes = p.data + (size_t)page * p.page_bytes + (size_t)h * 2 * PAGE * dh;
+  float* scale = p.scale + (size_t)page * p.page_scales + 2 * h;
+  const float old[2] = {scale[0], scale[1]};
+  __syncthreads();  // every thread has the old scales
+#pragma unroll
+  for (int side = 0; side < 2; ++side) {
+    float s = scale_of(fmaxf(fmaxf(red[side][0], red[side][1]), fmaxf(red[side][2], red[side][3])));
+    const int before = lo - start;  // earlier positions of the row on this page
+    uint8_t* c = codes + side * PAGE * dh;
+    if (before > 0) {
+      if (s > old[side]) {  // the codes of the earlier positions at the larger scale
+        const float f = old[side] / s;
+        for (int i = threadIdx.x; i < before * dh; i += 256) {
+          uint8_t* at = side == 0 ? c + i : c + (i / before) * PAGE + i % before;
+          *at = (uint8_t)(__builtin_amdgcn_cvt_pk_fp8_f32(value_of(*at) * f, 0.f, 0, false) & 255);
+        }
+      } else {
+        s = old[side];
+      }
+    }
+    const float inv = 1.f / s;
+    for (int i = threadIdx.x; i < m * dh; i += 256) {
+      if (side == 0)
+        c[(size_t)before * dh + i] = code_of(f32_of(ks[i]), inv);
+      else
+        c[(i / m) * PAGE + before + i % m] = code_of(f32_of(vs[(size_t)(i / m) * cap + i % m]), inv);
+    }
+    if (threadIdx.x == 0) scale[side] = s;
+  }
+}
+
+// One block per (page of a row, K/V head, row).
+template <class T>
+__global__ __launch_bounds__(256) void read_kernel(PageLayer p, PageRows r, T* k, T* vt, int cap) {
+  const int b = blockIdx.z, h = blockIdx.y, dh = p.dh;
+  const int start = blockIdx.x * PAGE, m = min(row_len(r, b) - start, PAGE);
+  if (m <= 0) return;
+  const int page = r.table[(size_t)b * r.max_pages + blockIdx.x];
+  const bool there = (unsigned)page < (unsigned)p.n_pages;
+  const uint8_t* codes = p.data + (size_t)(there ? page : 0) * p.page_bytes + (size_t)h * 2 * PAGE * dh;
+  const float* scale = p.scale + (size_t)(there ? page : 0) * p.page_scales + 2 * h;
+  const float sk = scale[0], sv = scale[1];
+  T* kd = k + (((size_t)b * p.Hkv + h) * cap + start) * dh;
+  T* vd = vt + ((size_t)b * p.Hkv + h) * dh * cap + start;
+  for (int i = threadIdx.x; i < m * dh; i += 256) {
+    kd[i] = from_f32<T>(there ? value_of(codes[i]) * sk : 0.f);
+    const int d = i / m, j = i % m;
+    vd[(size_t)d * cap + j] = from_f32<T>(there ? value_of(codes[PAGE * dh + d * PAGE + j]) * sv : 0.f);
+  }
+}
+
+constexpr int COPY_PAIRS = 448;  // pairs of a launch: they travel in its arguments (4 KB)
+struct CopyPairs {
+  int32_t src[COPY_PAIRS], dst[COPY_PAIRS];
+};
+
+// grid: x = 16 KB pieces of a page, y = pairs.
+__global__ __launch_bounds__(256) void copy_pages_kernel(uint8_t* data, float* scale, size_t page_bytes,
+                                                         size_t page_scales, CopyPairs pairs) {
+  const int src = pairs.src[blockIdx.y], dst = pairs.dst[blockIdx.y];
+  const uint4* a = reinterpret_cast<const uint4*>(data + (size_t)src * page_bytes);
+  uint4* o = reinterpret_cast<uint4*>(data + (size_t)dst * page_bytes);
+  const size_t n = page_bytes / 16, first = (size_t)blockIdx.x * 1024 + threadIdx.x;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (first + 256 * i < n) o[first + 256 * i] = a[first + 256 * i];
+  if (blockIdx.x == 0)
+    for (size_t i = threadIdx.x; i < page_scales; i += 256)
+      scale[(size_t)dst * page_scales + i] = scale[(size_t)src * page_scales + i];
+}
+
+__global__ __launch_bounds__(512) void table_set_kernel(int32_t* table, CopyPairs pairs, int n) {
+  const int i = threadIdx.x;
+  if (i < n) table[pairs.src[i]] = pairs.dst[i];
+}
+
+// pairs [i, i + COPY_PAIRS) of two lists of n, unused places 0
+CopyPairs some_pairs(const int32_t* a, const int32_t* b, int i, int n, int* m) {
+  CopyPairs pairs{};
+  *m = n - i < COPY_PAIRS ? n - i : COPY_PAIRS;
+  for (int j = 0; j < *m; ++j) {
+    pairs.src[j] = a[i + j];
+    pairs.dst[j] = b[i + j];
+  }
+  return pairs;
+}
+
+}  // namespace
+
+hipError_t table_set(int32_t* table, const int32_t* at, const int32_t* id, int n, hipStream_t s) {
+  for (int i = 0, m; i < n; i += COPY_PAIRS) {
+    const CopyPairs pairs = some_pairs(at, id, i, n, &m);
+    hipLaunchKernelGGL(table_set_kernel, dim3(1), dim3(512), 0, s, table, pairs, m);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+hipError_t pages_append(DType dt, const PageLayer& p, const PageRows& r, const void* k, const void* vt, int cap,
+                        hipStream_t s) {
+  const dim3 grid((r.max_n + PAGE - 1) / PAGE + 1, p.Hkv, r.B);
+  if (dt == BF16)
+    hipLaunchKernelGGL(append_kernel<bf16>, grid, dim3(256), 0, s, p, r, static_cast<const bf16*>(k),
+                       static_cast<const bf16*>(vt), cap);
+  else
+    hipLaunchKernelGGL(append_kernel<float>, grid, dim3(256), 0, s, p, r, static_cast<const float*>(k),
+                       static_cast<const float*>(vt), cap);
+  return hipGetLastError();
+}
+
+hipError_t pages_read(DType dt, const PageLayer& p, const PageRows& r, void* k, void* vt, int cap, hipStream_t s) {
+  const dim3 grid((r.max_len + PAGE - 1) / PAGE, p.Hkv, r.B);
+  if (grid.x == 0) return hipSuccess;
+  if (dt == BF16)
+    hipLaunchKernelGGL(read_kernel<bf16>, grid, dim3(256), 0, s, p, r, static_cast<bf16*>(k), static_cast<bf16*>(vt),
+                       cap);
+  else
+    hipLaunchKernelGGL(read_kernel<float>, grid, dim3(256), 0, s, p, r, static_cast<float*>(k),
+                       static_cast<float*>(vt), cap);
+  return hipGetLastError();
+}
+
+hipError_t pages_copy(void* data, float* scale, size_t page_bytes, size_t page_scales, const int32_t* src,
+                      const int32_t* dst, int n, hipStream_t s) {
+  const unsigned pieces = (unsigned)((page_bytes + 16383) / 16384);
+  for (int i = 0, m; i < n; i += COPY_PAIRS) {
+    const CopyPairs pairs = some_pairs(src, dst, i, n, &m);
+    hipLaunchKernelGGL(copy_pages_kernel, dim3(pieces, m), dim3(256), 0, s, static_cast<uint8_t*>(data), scale,
+                       page_bytes, page_scales, pairs);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+}  // namespace tadm

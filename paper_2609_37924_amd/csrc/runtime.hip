@@ -19,6 +19,8 @@
 
 #include "../../include/tadm.h"
 #include "kernels.h"
+#include "page_book.h"
+#include "pages.h"
 
 using namespace tadm;
 
@@ -314,10 +316,27 @@ struct tadm_cache {
   int refresh_i = 0;
 };
 
+// Pages of a model and who holds them.  Page ids travel by value in kernel arguments and
+// everything runs on the model's stream, so host state may run ahead of the device.
+struct tadm_pool {
+  tadm_model* model;
+  PageBook book;
+  uint8_t* data = nullptr;
+  float* scale = nullptr;
+  std::vector<tadm_context*> contexts;
+};
+
 struct tadm_context {
   tadm_model* model;
   int B, cap, len = 0;
   std::vector<void*> k, vt;  // per layer [B, Hkv, cap, dh] / [B, Hkv, dh, cap]
+  // pooled: the pages of each row, [B, cap / PAGE] on the host and the device
+  tadm_pool* pool = nullptr;
+  PageTable table;
+  int32_t* table_dev = nullptr;
+  void* work = nullptr;  // scratch of the attention: the most that any window needs
+  size_t work_bytes = 0;
+  bool appending = false;  // the running pass commits its K, V
 };
 
 // ---------------------------------------------------------------- profiling ---
@@ -472,7 +491,20 @@ static tadm_status ensure_kpart(tadm_model* m, size_t floats) {
 struct KVTarget {
   void *k, *vt;
   int cap, off;
+  const tadm_context* pages = nullptr;  // the committed positions are on pages; k, vt: the window alone
 };
+
+static PageLayer pool_layer(const tadm_pool* p, int li) {
+  const tadm_config& c = p->model->cfg;
+  const int nl = p->model->n_layers();
+  const size_t layer = (size_t)c.n_kv_heads * 2 * PAGE * c.head_dim;
+  return PageLayer{p->data + li * layer, p->scale + (size_t)li * 2 * c.n_kv_heads, nl * layer,
+                   (size_t)nl * 2 * c.n_kv_heads, p->book.size(), c.n_kv_heads, c.head_dim};
+}
+
+static PageRows context_rows(const tadm_context* x, int n) {
+  return PageRows{x->table_dev, nullptr, nullptr, x->B, x->table.per_row, x->len, n};
+}
 
 // One pre-norm layer on x [N, d]; prenormed: ws.xn already holds the attention norm of x.
 // next_norm: the attention-norm gains of the layer that follows (nullptr if none); when
@@ -515,8 +547,15 @@ static tadm_status run_layer(tadm_model* m, int li, float* x, int B, int L, int 
     HIPCHK(gemm(m->dt, p, EPI_QKV_ROPE, e, st));
     TRY(prof_end(m, TADM_STAGE_QKV));
   }
-  TRY(prof_begin(m, TADM_STAGE_ATTN));
-  HIPCHK(attention(m->dt, s.q, kv.k, kv.vt, s.ao, B, H, Hk, L, kv.off + L, kv.cap, dh, st));
+  TRY(prof_begin(m, TADM_STAGE_ATTN, kv.pages != nullptr));
+  if (kv.pages) {
+    const PageLayer pl = pool_layer(kv.pages->pool, li);
+    const PageRows rows = context_rows(kv.pages, L);
+    HIPCHK(page_attend(m->dt, PageAttend{pl, rows, s.q, kv.k, kv.vt, s.ao, nullptr, H, kv.cap, kv.pages->work}, st));
+    if (kv.pages->appending) HIPCHK(pages_append(m->dt, pl, rows, kv.k, kv.vt, kv.cap, st));
+  } else {
+    HIPCHK(attention(m->dt, s.q, kv.k, kv.vt, s.ao, B, H, Hk, L, kv.off + L, kv.cap, dh, st));
+  }
   TRY(prof_end(m, TADM_STAGE_ATTN));
   {
     GemmProblem p{N, d, H * dh, s.ao, H * dh, H * dh, nullptr, 0, m->W(w.wo), H * dh};
@@ -589,6 +628,7 @@ static tadm_status run_layer(tadm_model* m, int li, float* x, int B, int L, int 
 }
 
 static KVTarget kv_target(tadm_model* m, const tadm_context* ctx, int li) {
+  if (ctx && ctx->pool) return KVTarget{m->ws.k, m->ws.vt, m->ws.kv_cap, 0, ctx};
   if (ctx) return KVTarget{ctx->k[li], ctx->vt[li], ctx->cap, ctx->len};
   return KVTarget{m->ws.k, m->ws.vt, m->ws.kv_cap, 0};
 }
@@ -1161,6 +1201,35 @@ tadm_status tadm_cache_read(const tadm_cache* c, int32_t field, void* dst_dev, s
 int32_t tadm_cache_refresh_step(const tadm_cache* c) { return c ? c->refresh_i : 0; }
 
 // ---------------------------------------------------------------- context ---
+}  // extern "C"
+
+// Keeps the positions [0, len): a pooled context gives back the pages that hold no others.
+static void context_drop(tadm_context* x, int len) {
+  x->len = len;
+  if (x->pool) x->pool->book.drop(x->table, (len + PAGE - 1) / PAGE);
+}
+
+// Gives every row of a pooled context pages of its own for the positions [len, len + n).
+// Nothing has changed when it fails for want of pages.
+static tadm_status pages_take(tadm_context* x, int n) {
+  tadm_pool* p = x->pool;
+  PageMoves mv;
+  try {
+    if (!p->book.own(x->table, x->len / PAGE, (x->len + n - 1) / PAGE, mv))
+      return fail(TADM_ERR_OOM, "%zu pages needed, %zu of the pool's %d are free", mv.at.size(), p->book.free.size(),
+                  p->book.size());
+  } catch (const std::exception&) {
+    return fail(TADM_ERR_OOM, "host memory");
+  }
+  const PageLayer pl = pool_layer(p, 0);
+  HIPCHK(pages_copy(p->data, p->scale, pl.page_bytes, pl.page_scales, mv.src.data(), mv.dst.data(), (int)mv.src.size(),
+                    x->model->stream));
+  HIPCHK(table_set(x->table_dev, mv.at.data(), mv.to.data(), (int)mv.at.size(), x->model->stream));
+  return TADM_OK;
+}
+
+extern "C" {
+
 tadm_status tadm_context_create(tadm_model* m, int32_t B, int32_t max_ctx, tadm_context** out) {
   if (!m || !out) return fail(TADM_ERR_INVALID, "null argument");
   *out = nullptr;
@@ -1191,7 +1260,14 @@ int32_t tadm_context_length(const tadm_context* ctx) { return ctx ? ctx->len : 0
 
 tadm_status tadm_context_reset(tadm_context* ctx) {
   if (!ctx) return fail(TADM_ERR_INVALID, "null context");
-  ctx->len = 0;
+  context_drop(ctx, 0);
+  return TADM_OK;
+}
+
+tadm_status tadm_context_truncate(tadm_context* ctx, int32_t len) {
+  if (!ctx) return fail(TADM_ERR_INVALID, "null context");
+  if (len < 0 || len > ctx->len) return fail(TADM_ERR_INVALID, "length %d of a context of %d positions", len, ctx->len);
+  context_drop(ctx, len);
   return TADM_OK;
 }
 
@@ -1200,7 +1276,370 @@ tadm_status tadm_context_destroy(tadm_context* ctx) {
   (void)hipDeviceSynchronize();
   for (void* p : ctx->k) (void)hipFree(p);
   for (void* p : ctx->vt) (void)hipFree(p);
+  if (ctx->pool) {
+    context_drop(ctx, 0);
+    auto& all = ctx->pool->contexts;
+    all.erase(std::remove(all.begin(), all.end(), ctx), all.end());
+  }
+  if (ctx->table_dev) (void)hipFree(ctx->table_dev);
+  if (ctx->work) (void)hipFree(ctx->work);
   delete ctx;
+  return TADM_OK;
+}
+
+// ----------------------------------------------------- paged 8-bit K/V ---
+}  // extern "C"
+
+// The model's device for the duration of a call.
+namespace {
+struct OnDevice {
+  int prev = -1;
+  hipError_t err;
+  explicit OnDevice(int device) {
+    err = hipGetDevice(&prev);
+    if (err == hipSuccess && prev != device)
+      err = hipSetDevice(device);
+    else
+      prev = -1;
+  }
+  ~OnDevice() {
+    if (prev >= 0) (void)hipSetDevice(prev);
+  }
+};
+
+bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
+}  // namespace
+
+// The arguments are checked before the model, so that a call without one names what is wrong with them.
+static tadm_status check_pages(const tadm_pages* p, int layer) {
+  if (!p || !p->data || !p->scale) return fail(TADM_ERR_INVALID, "null pages");
+  if (p->n_pages < 1 || p->n_layers < 1 || p->n_kv_heads < 1 || p->head_dim < 1)
+    return fail(TADM_ERR_INVALID, "%d pages of %d layers of %d heads x %d", p->n_pages, p->n_layers, p->n_kv_heads,
+                p->head_dim);
+  if (!aligned(p->data, 16) || !aligned(p->scale, 4)) return fail(TADM_ERR_INVALID, "pages not aligned to 16 bytes");
+  if (layer < 0 || layer >= p->n_layers) return fail(TADM_ERR_INVALID, "layer %d of %d", layer, p->n_layers);
+  return TADM_OK;
+}
+
+static tadm_status check_page_model(const tadm_model* m, const tadm_pages* p) {
+  if (!m) return fail(TADM_ERR_INVALID, "null model");
+  if (p->n_kv_heads != m->cfg.n_kv_heads || p->head_dim != m->cfg.head_dim)
+    return fail(TADM_ERR_INVALID, "pages of %d heads x %d, model of %d x %d", p->n_kv_heads, p->head_dim,
+                m->cfg.n_kv_heads, m->cfg.head_dim);
+  return TADM_OK;
+}
+
+static tadm_status check_rows(const tadm_page_rows* r) {
+  if (!r || !r->table_dev) return fail(TADM_ERR_INVALID, "null rows or table");
+  if (r->B < 1 || r->B > 65535) return fail(TADM_ERR_INVALID, "B=%d outside [1, 65535]", r->B);
+  if (r->max_pages < 1 || r->max_pages > (1 << 24)) return fail(TADM_ERR_INVALID, "max_pages=%d", r->max_pages);
+  if (r->len < 0 || r->len > (long)r->max_pages * PAGE)
+    return fail(TADM_ERR_INVALID, "%d positions with %d pages a row", r->len, r->max_pages);
+  if (!aligned(r->table_dev, 4) || !aligned(r->len_dev, 4) || !aligned(r->n_dev, 4))
+    return fail(TADM_ERR_INVALID, "table or lengths not aligned to 4 bytes");
+  return TADM_OK;
+}
+
+// A window's K, V^T arrays with n tokens.
+static tadm_status check_window_kv(const void* k, const void* vt, int n, int cap) {
+  if (!k || !vt) return fail(TADM_ERR_INVALID, "null keys or values");
+  if (cap < n || cap % 64) return fail(TADM_ERR_INVALID, "cap=%d must be a multiple of 64 and hold %d tokens", cap, n);
+  if (!aligned(k, 16) || !aligned(vt, 16)) return fail(TADM_ERR_INVALID, "keys or values not aligned to 16 bytes");
+  return TADM_OK;
+}
+
+static PageLayer page_layer(const tadm_pages* p, int layer) {
+  const size_t bytes = (size_t)p->n_kv_heads * 2 * PAGE * p->head_dim;
+  return PageLayer{static_cast<uint8_t*>(p->data) + layer * bytes, p->scale + (size_t)layer * 2 * p->n_kv_heads,
+                   p->n_layers * bytes, (size_t)p->n_layers * 2 * p->n_kv_heads, p->n_pages, p->n_kv_heads, p->head_dim};
+}
+
+static PageRows page_rows(const tadm_page_rows* r, int n) {
+  return PageRows{r->table_dev, r->len_dev, r->n_dev, r->B, r->max_pages, r->len, n};
+}
+
+extern "C" {
+
+tadm_status tadm_pages_append(tadm_model* m, const tadm_pages* p, int32_t layer, const tadm_page_rows* rows,
+                              const void* k_dev, const void* vt_dev, int32_t n, int32_t cap) {
+  TRY(check_pages(p, layer));
+  TRY(check_rows(rows));
+  if (n < 1) return fail(TADM_ERR_INVALID, "n=%d", n);
+  TRY(check_window_kv(k_dev, vt_dev, n, cap));
+  if (!rows->len_dev && (long)rows->len + n > (long)rows->max_pages * PAGE)
+    return fail(TADM_ERR_INVALID, "positions [%d, %ld) with %d pages a row", rows->len, (long)rows->len + n, rows->max_pages);
+  TRY(check_page_model(m, p));
+  OnDevice dev(m->device);
+  HIPCHK(dev.err);
+  HIPCHK(pages_append(m->dt, page_layer(p, layer), page_rows(rows, n), k_dev, vt_dev, cap, m->stream));
+  return TADM_OK;
+}
+
+static tadm_status check_queries(const tadm_model* m, const tadm_page_rows* rows, int n) {
+  if (!m) return fail(TADM_ERR_INVALID, "null model");
+  if ((int64_t)rows->B * m->cfg.n_heads * n > INT32_MAX)
+    return fail(TADM_ERR_INVALID, "%d rows of %d queries: too many in one call", rows->B, n);
+  return TADM_OK;
+}
+
+size_t tadm_pages_attend_work(const tadm_model* m, const tadm_page_rows* rows, int32_t n) {
+  if (check_rows(rows) != TADM_OK || n < 1 || check_queries(m, rows, n) != TADM_OK) return 0;
+  return page_attend_work(m->dt, rows->B, m->cfg.n_heads, m->cfg.n_kv_heads, m->cfg.head_dim, n, rows->len);
+}
+
+tadm_status tadm_pages_attend(tadm_model* m, const tadm_pages* p, int32_t layer, const tadm_page_rows* rows,
+                              const void* q_dev, int32_t n, const void* k_dev, const void* vt_dev, int32_t cap,
+                              void* o_dev, float* lse_dev, void* work_dev, size_t work_bytes) {
+  TRY(check_pages(p, layer));
+  TRY(check_rows(rows));
+  if (n < 1) return fail(TADM_ERR_INVALID, "n=%d", n);
+  if (!q_dev || !o_dev) return fail(TADM_ERR_INVALID, "null queries or output");
+  if (!aligned(q_dev, 16) || !aligned(o_dev, 16) || !aligned(lse_dev, 4))
+    return fail(TADM_ERR_INVALID, "queries or output not aligned to 16 bytes");
+  if (k_dev || vt_dev) TRY(check_window_kv(k_dev, vt_dev, n, cap));
+  TRY(check_queries(m, rows, n));
+  TRY(check_page_model(m, p));
+  const size_t need = tadm_pages_attend_work(m, rows, n);
+  if (need && (!work_dev || work_bytes < need || !aligned(work_dev, 16)))
+    return fail(TADM_ERR_INVALID, "scratch of %zu bytes, %zu needed, aligned to 16", work_dev ? work_bytes : 0, need);
+  OnDevice dev(m->device);
+  HIPCHK(dev.err);
+  HIPCHK(page_attend(m->dt, PageAttend{page_layer(p, layer), page_rows(rows, n), q_dev, k_dev, vt_dev, o_dev, lse_dev,
+                                       m->cfg.n_heads, cap, work_dev}, m->stream));
+  return TADM_OK;
+}
+
+tadm_status tadm_pages_read(tadm_model* m, const tadm_pages* p, int32_t layer, const tadm_page_rows* rows,
+                            void* k_dev, void* vt_dev, int32_t cap) {
+  TRY(check_pages(p, layer));
+  TRY(check_rows(rows));
+  TRY(check_window_kv(k_dev, vt_dev, rows->len, cap));
+  TRY(check_page_model(m, p));
+  OnDevice dev(m->device);
+  HIPCHK(dev.err);
+  HIPCHK(pages_read(m->dt, page_layer(p, layer), page_rows(rows, 0), k_dev, vt_dev, cap, m->stream));
+  return TADM_OK;
+}
+
+tadm_status tadm_pages_copy(tadm_model* m, const tadm_pages* p, const int32_t* src, const int32_t* dst,
+                            int32_t n_copies) {
+  TRY(check_pages(p, 0));
+  if (n_copies < 0 || n_copies > p->n_pages) return fail(TADM_ERR_INVALID, "%d copies in %d pages", n_copies, p->n_pages);
+  if (n_copies && (!src || !dst)) return fail(TADM_ERR_INVALID, "null page list");
+  try {
+    std::vector<int32_t> d(dst, dst + n_copies);
+    std::sort(d.begin(), d.end());
+    if (n_copies && (d.front() < 0 || d.back() >= p->n_pages))
+      return fail(TADM_ERR_INVALID, "destination outside [0, %d)", p->n_pages);
+    if (std::adjacent_find(d.begin(), d.end()) != d.end()) return fail(TADM_ERR_INVALID, "a destination appears twice");
+    for (int i = 0; i < n_copies; ++i) {
+      if (src[i] < 0 || src[i] >= p->n_pages) return fail(TADM_ERR_INVALID, "source page %d of %d", src[i], p->n_pages);
+      if (std::binary_search(d.begin(), d.end(), src[i]))
+        return fail(TADM_ERR_INVALID, "page %d is a source and a destination", src[i]);
+    }
+  } catch (const std::exception&) {
+    return fail(TADM_ERR_OOM, "host memory");
+  }
+  TRY(check_page_model(m, p));
+  OnDevice dev(m->device);
+  HIPCHK(dev.err);
+  const PageLayer pl = page_layer(p, 0);
+  HIPCHK(pages_copy(p->data, p->scale, pl.page_bytes, pl.page_scales, src, dst, n_copies, m->stream));
+  return TADM_OK;
+}
+
+// ------------------------------------------------------------------- pool ---
+tadm_status tadm_pool_create(tadm_model* m, int32_t n_pages, tadm_pool** out) {
+  if (!m || !out) return fail(TADM_ERR_INVALID, "null argument");
+  *out = nullptr;
+  if (n_pages < 1 || m->n_layers() < 1) return fail(TADM_ERR_INVALID, "%d pages of %d layers", n_pages, m->n_layers());
+  OnDevice dev(m->device);
+  HIPCHK(dev.err);
+  tadm_pool* p = nullptr;
+  try {
+    p = new tadm_pool{m, PageBook(n_pages)};
+  } catch (const std::exception&) {
+    return fail(TADM_ERR_OOM, "host memory");
+  }
+  const PageLayer pl = pool_layer(p, 0);
+  hipError_t e = hipMalloc((void**)&p->data, (size_t)n_pages * pl.page_bytes);
+  if (e == hipSuccess) e = hipMalloc((void**)&p->scale, (size_t)n_pages * pl.page_scales * 4);
+  if (e != hipSuccess) {
+    if (p->data) (void)hipFree(p->data);
+    const size_t bytes = (size_t)n_pages * pl.page_bytes;
+    delete p;
+    return fail(e == hipErrorOutOfMemory ? TADM_ERR_OOM : TADM_ERR_DEVICE, "pool (%zu bytes): %s", bytes,
+                hipGetErrorString(e));
+  }
+  *out = p;
+  return TADM_OK;
+}
+
+tadm_status tadm_pool_destroy(tadm_pool* pool) {
+  if (!pool) return fail(TADM_ERR_INVALID, "null pool");
+  if (!pool->contexts.empty()) return fail(TADM_ERR_STATE, "%zu contexts still use the pool", pool->contexts.size());
+  (void)hipDeviceSynchronize();
+  (void)hipFree(pool->data);
+  (void)hipFree(pool->scale);
+  delete pool;
+  return TADM_OK;
+}
+
+int32_t tadm_pool_size(const tadm_pool* pool) { return pool ? pool->book.size() : 0; }
+int32_t tadm_pool_free_pages(const tadm_pool* pool) { return pool ? pool->book.size() - pool->book.held() : 0; }
+
+tadm_status tadm_pool_pages(const tadm_pool* pool, tadm_pages* out) {
+  if (!pool || !out) return fail(TADM_ERR_INVALID, "null argument");
+  const tadm_config& c = pool->model->cfg;
+  *out = tadm_pages{pool->data, pool->scale, pool->book.size(), pool->model->n_layers(), c.n_kv_heads, c.head_dim};
+  return TADM_OK;
+}
+
+tadm_status tadm_pool_compact(tadm_pool* pool) {
+  if (!pool) return fail(TADM_ERR_INVALID, "null pool");
+  tadm_model* m = pool->model;
+  OnDevice dev(m->device);
+  HIPCHK(dev.err);
+  try {
+    PageMoves mv;
+    std::vector<int32_t> to;
+    size_t most = 0;  // no allocation once pages have moved
+    for (const tadm_context* x : pool->contexts) most = std::max(most, x->table.id.size());
+    mv.src.reserve(pool->book.held());
+    mv.dst.reserve(pool->book.held());
+    mv.at.reserve(most);
+    mv.to.reserve(most);
+    pool->book.compact(mv, to);
+    const PageLayer pl = pool_layer(pool, 0);
+    HIPCHK(pages_copy(pool->data, pool->scale, pl.page_bytes, pl.page_scales, mv.src.data(), mv.dst.data(),
+                      (int)mv.src.size(), m->stream));
+    if (mv.src.empty()) return TADM_OK;
+    for (tadm_context* x : pool->contexts) {
+      PageBook::renumber(x->table, to, mv);
+      HIPCHK(table_set(x->table_dev, mv.at.data(), mv.to.data(), (int)mv.at.size(), m->stream));
+    }
+  } catch (const std::exception&) {
+    return fail(TADM_ERR_OOM, "host memory");
+  }
+  return TADM_OK;
+}
+
+tadm_status tadm_pool_resize(tadm_pool* pool, int32_t n_pages) {
+  if (!pool) return fail(TADM_ERR_INVALID, "null pool");
+  const int held = pool->book.held();
+  if (n_pages < 1 || n_pages < held) return fail(TADM_ERR_INVALID, "%d pages, %d are held", n_pages, held);
+  OnDevice dev(pool->model->device);
+  HIPCHK(dev.err);
+  try {
+    pool->book.refs.reserve(n_pages);
+    pool->book.free.reserve(n_pages);
+  } catch (const std::exception&) {
+    return fail(TADM_ERR_OOM, "host memory");
+  }
+  TRY(tadm_pool_compact(pool));
+  const PageLayer pl = pool_layer(pool, 0);
+  uint8_t* data = nullptr;
+  float* scale = nullptr;
+  hipError_t e = hipMalloc((void**)&data, (size_t)n_pages * pl.page_bytes);
+  if (e == hipSuccess) e = hipMalloc((void**)&scale, (size_t)n_pages * pl.page_scales * 4);
+  if (e == hipSuccess && held)
+    e = hipMemcpyAsync(data, pool->data, (size_t)held * pl.page_bytes, hipMemcpyDeviceToDevice, pool->model->stream);
+  if (e == hipSuccess && held)
+    e = hipMemcpyAsync(scale, pool->scale, (size_t)held * pl.page_scales * 4, hipMemcpyDeviceToDevice,
+                       pool->model->stream);
+  if (e == hipSuccess) e = hipDeviceSynchronize();
+  if (e != hipSuccess) {
+    if (data) (void)hipFree(data);
+    if (scale) (void)hipFree(scale);
+    return fail(e == hipErrorOutOfMemory ? TADM_ERR_OOM : TADM_ERR_DEVICE, "pool of %d pages: %s", n_pages,
+                hipGetErrorString(e));
+  }
+  (void)hipFree(pool->data);
+  (void)hipFree(pool->scale);
+  pool->data = data;
+  pool->scale = scale;
+  pool->book.resize(n_pages);
+  return TADM_OK;
+}
+
+}  // extern "C"
+
+// A pooled context without pages; its scratch covers every window that its positions allow.
+static tadm_status pooled_create(tadm_pool* pool, int B, int cap, tadm_context** out) {
+  tadm_model* m = pool->model;
+  OnDevice dev(m->device);
+  HIPCHK(dev.err);
+  tadm_context* x = nullptr;
+  try {
+    x = new tadm_context();
+    x->model = m;
+    x->B = B;
+    x->cap = cap;
+    x->table = PageTable(B, cap / PAGE);
+    pool->contexts.push_back(x);
+  } catch (const std::exception&) {
+    delete x;
+    return fail(TADM_ERR_OOM, "host memory");
+  }
+  x->pool = pool;
+  for (int n = 1; n <= m->cfg.max_seq; ++n)
+    for (int len : {0, cap})
+      x->work_bytes = std::max(x->work_bytes, page_attend_work(m->dt, B, m->cfg.n_heads, m->cfg.n_kv_heads,
+                                                               m->cfg.head_dim, n, len));
+  hipError_t e = hipMalloc((void**)&x->table_dev, x->table.id.size() * 4);
+  if (e == hipSuccess) e = hipMalloc(&x->work, std::max<size_t>(x->work_bytes, 256));
+  if (e != hipSuccess) {
+    tadm_context_destroy(x);
+    return fail(e == hipErrorOutOfMemory ? TADM_ERR_OOM : TADM_ERR_DEVICE, "context: %s", hipGetErrorString(e));
+  }
+  *out = x;
+  return TADM_OK;
+}
+
+extern "C" {
+
+tadm_status tadm_context_create_pooled(tadm_model* m, tadm_pool* pool, int32_t B, int32_t max_ctx,
+                                       tadm_context** out) {
+  if (!m || !pool || !out) return fail(TADM_ERR_INVALID, "null argument");
+  *out = nullptr;
+  if (pool->model != m) return fail(TADM_ERR_STATE, "pool belongs to another model");
+  if (B < 1 || B > m->cfg.max_batch || max_ctx < 1 || max_ctx > m->cfg.max_seq)
+    return fail(TADM_ERR_INVALID, "context shape B=%d max_ctx=%d outside the model limits", B, max_ctx);
+  return pooled_create(pool, B, round64(max_ctx), out);
+}
+
+tadm_status tadm_context_fork(const tadm_context* src, const int32_t* rows, int32_t B, tadm_context** out) {
+  if (!src || !rows || !out) return fail(TADM_ERR_INVALID, "null argument");
+  *out = nullptr;
+  if (!src->pool) return fail(TADM_ERR_STATE, "only pooled contexts can be forked");
+  tadm_model* m = src->model;
+  if (B < 1 || B > m->cfg.max_batch) return fail(TADM_ERR_INVALID, "B=%d outside [1, %d]", B, m->cfg.max_batch);
+  for (int b = 0; b < B; ++b)
+    if (rows[b] < 0 || rows[b] >= src->B) return fail(TADM_ERR_INVALID, "row %d of a context of %d rows", rows[b], src->B);
+  tadm_context* x = nullptr;
+  TRY(pooled_create(src->pool, B, src->cap, &x));
+  const int held = (src->len + PAGE - 1) / PAGE;
+  OnDevice dev(m->device);
+  hipError_t e = dev.err;
+  for (int b = 0; b < B && e == hipSuccess; ++b) {
+    x->pool->book.share(src->table, rows[b], x->table, b, held);
+    if (held)
+      e = hipMemcpyAsync(x->table_dev + (size_t)b * x->table.per_row, src->table_dev + (size_t)rows[b] * x->table.per_row,
+                         (size_t)held * 4, hipMemcpyDeviceToDevice, m->stream);
+  }
+  x->len = src->len;
+  if (e != hipSuccess) {
+    tadm_context_destroy(x);
+    return fail(TADM_ERR_DEVICE, "fork: %s", hipGetErrorString(e));
+  }
+  *out = x;
+  return TADM_OK;
+}
+
+tadm_status tadm_context_rows(const tadm_context* ctx, tadm_page_rows* out) {
+  if (!ctx || !out) return fail(TADM_ERR_INVALID, "null argument");
+  if (!ctx->pool) return fail(TADM_ERR_STATE, "the context has no pages");
+  *out = tadm_page_rows{ctx->table_dev, nullptr, nullptr, ctx->B, ctx->table.per_row, ctx->len};
   return TADM_OK;
 }
 
@@ -1209,6 +1648,11 @@ tadm_status tadm_context_destroy(tadm_context* ctx) {
 static tadm_status context_append_impl(tadm_model* m, tadm_context* ctx, const int32_t* tok, int B,
                                        int n, tadm_cache* scratch) {
   Workspace& s = m->ws;
+  struct Appending {  // every layer of this pass commits its K, V to the pages
+    tadm_context* x;
+    ~Appending() { x->appending = false; }
+  } appending{ctx};
+  ctx->appending = true;
   TRY(shared_anchor(m, ctx, tok, B, n, nullptr, 0, scratch, false));
   bool prenormed;
   TRY(fusion(m, B, n, scratch->c, scratch, false, &prenormed));
@@ -1229,6 +1673,7 @@ tadm_status tadm_context_append(tadm_model* m, tadm_context* ctx, const int32_t*
   TRY(check_window(m, ctx, B, n));
   TRY(ensure_workspace(m));
   TRY(ensure_scratch(m));
+  if (ctx->pool) TRY(pages_take(ctx, n));
   TRY(prof_begin(m, TADM_STAGE_CONTEXT));
   TRY(context_append_impl(m, ctx, tokens_dev, B, n, m->scratch));
   return prof_end(m, TADM_STAGE_CONTEXT);
@@ -1800,6 +2245,10 @@ tadm_status tadm_context_read(const tadm_context* ctx, int32_t layer, void* k_de
   if (layer < 0 || layer >= m->n_layers()) return fail(TADM_ERR_INVALID, "layer %d", layer);
   const size_t n = (size_t)ctx->B * m->cfg.n_kv_heads * ctx->cap * m->cfg.head_dim * m->esz;
   if (bytes != n) return fail(TADM_ERR_INVALID, "context layer has %zu bytes, got %zu", n, bytes);
+  if (ctx->pool) {
+    if (ctx->len) HIPCHK(pages_read(m->dt, pool_layer(ctx->pool, layer), context_rows(ctx, 0), k_dev, vt_dev, ctx->cap, m->stream));
+    return TADM_OK;
+  }
   HIPCHK(hipMemcpyAsync(k_dev, ctx->k[layer], n, hipMemcpyDeviceToDevice, m->stream));
   HIPCHK(hipMemcpyAsync(vt_dev, ctx->vt[layer], n, hipMemcpyDeviceToDevice, m->stream));
   return TADM_OK;
