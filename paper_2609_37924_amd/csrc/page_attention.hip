@@ -29,7 +29,7 @@ struct Args {
   const void *q, *k, *vt;
   void* o;
   float* lse;
-  float* part;  // per (row, K/V head, column, split): dh values of O, then m and l
+  float* part;  // S > 1: O [row, K/V head, column, split, dh], then (m, l) [row, K/V head, column, split, 2]
   int G, cap, S;
   float scale_log2;
 };
@@ -45,6 +45,13 @@ __device__ __forceinline__ int row_new(const PageRows& r, int b) {
 __device__ __forceinline__ f32x4 f32_codes(uint32_t c, float s) {
   const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)c, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)c, true);
   return f32x4{lo[0] * s, lo[1] * s, hi[0] * s, hi[1] * s};
+}
+__device__ __forceinline__ float* part_o(const Args& a, size_t col, int split) {
+  return a.part + (col * a.S + split) * a.p.dh;
+}
+__device__ __forceinline__ float* part_ml(const Args& a, size_t col, int split) {
+  const size_t cols = (size_t)a.r.B * a.p.Hkv * a.G * a.r.max_n;
+  return a.part + cols * a.S * a.p.dh + (col * a.S + split) * 2;
 }
 // 8 codes as bf16 times the scale, exactly
 __device__ __forceinline__ bf16x8 bf16_codes(uint32_t a, uint32_t b, float s) {
@@ -281,7 +288,7 @@ __global__ __launch_bounds__(64 * NW) void attend_kernel(Args a) {
     const int col = ct * 16 * QS + 16 * u + fr, g = col / L, j = col % L;
     if (col >= ncol || j >= n) continue;
     const float inv = a.S > 1 ? 1.f : sum == 0.f ? 0.f : 1.f / sum;
-    float* part = a.part + ((head * ncol + col) * a.S + sp) * (dh + 2);
+    float* part = part_o(a, head * ncol + col, sp);
     T* out = static_cast<T*>(a.o) + (((size_t)b * L + j) * a.p.Hkv * a.G + h * a.G + g) * dh;
     for (int d = wave; d < NB; d += NW) {
       float r[4] = {0.f, 0.f, 0.f, 0.f};
@@ -291,8 +298,7 @@ __global__ __launch_bounds__(64 * NW) void attend_kernel(Args a) {
         for (int e = 0; e < 4; ++e) r[e] += x[(v * NV + 2 + 4 * d + e) * 64] * f[v];
       if (16 * d + 4 * grp < dh) {
         if (a.S > 1) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) part[16 * d + 4 * grp + e] = r[e];
+          store4(part + 16 * d + 4 * grp, r[0], r[1], r[2], r[3]);
         } else {
           store4(out + 16 * d + 4 * grp, r[0] * inv, r[1] * inv, r[2] * inv, r[3] * inv);
         }
@@ -300,8 +306,7 @@ __global__ __launch_bounds__(64 * NW) void attend_kernel(Args a) {
     }
     if (wave == 0 && grp == 0) {
       if (a.S > 1) {
-        part[dh] = m;
-        part[dh + 1] = sum;
+        store2(part_ml(a, head * ncol + col, sp), m, sum);
       } else if (a.lse) {
         a.lse[head * ncol + col] = sum == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * LN2;
       }
@@ -309,29 +314,49 @@ __global__ __launch_bounds__(64 * NW) void attend_kernel(Args a) {
   }
 }
 
-// Joins the splits of a column: one wave per (row, K/V head, column).
+// Joins the splits of a column, one block each: eight groups of 32 lanes take every eighth
+// split, four values of the head width a lane, and are summed in order.
 template <class T>
 __global__ __launch_bounds__(256) void join_kernel(Args a) {
-  const int lane = threadIdx.x & 63, L = a.r.max_n, ncol = a.G * L, dh = a.p.dh;
-  const size_t col_id = (size_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (col_id >= (size_t)a.r.B * a.p.Hkv * ncol) return;
+  __shared__ float xs[8][132];
+  const int lane = threadIdx.x & 63, g8 = threadIdx.x >> 5, i = threadIdx.x & 31;
+  const int L = a.r.max_n, ncol = a.G * L, dh = a.p.dh;
+  const size_t col_id = blockIdx.x;
   const int col = (int)(col_id % ncol), g = col / L, j = col % L;
   const int b = (int)(col_id / ncol / a.p.Hkv), h = (int)(col_id / ncol % a.p.Hkv);
   if (j >= row_new(a.r, b)) return;
-  const float* part = a.part + col_id * a.S * (dh + 2);
-  float m = -INFINITY, sum = 0.f;
-  for (int s = 0; s < a.S; ++s) m = fmaxf(m, part[(size_t)s * (dh + 2) + dh]);
+  const float* ml = part_ml(a, col_id, 0);
+  float m = -INFINITY;
+  for (int s = lane; s < a.S; s += 64) m = fmaxf(m, ml[2 * s]);
+  m = wave_max(m);
   const float ref = m == -INFINITY ? 0.f : m;
-  for (int s = 0; s < a.S; ++s)
-    sum += part[(size_t)s * (dh + 2) + dh + 1] * __builtin_amdgcn_exp2f(part[(size_t)s * (dh + 2) + dh] - ref);
-  const float inv = sum == 0.f ? 0.f : 1.f / sum;
-  T* out = static_cast<T*>(a.o) + (((size_t)b * L + j) * a.p.Hkv * a.G + h * a.G + g) * dh;
-  for (int d = lane; d < dh; d += 64) {
-    float r = 0.f;
-    for (int s = 0; s < a.S; ++s) r += part[(size_t)s * (dh + 2) + d] * __builtin_amdgcn_exp2f(part[(size_t)s * (dh + 2) + dh] - ref);
-    out[d] = from_f32<T>(r * inv);
+  const float* po = part_o(a, col_id, 0) + 4 * i;
+  float r[4] = {0.f, 0.f, 0.f, 0.f}, sum = 0.f;
+#pragma unroll 4
+  for (int s = g8; s < a.S; s += 8) {
+    const float f = __builtin_amdgcn_exp2f(ml[2 * s] - ref);
+    sum += ml[2 * s + 1] * f;
+    if (4 * i < dh) {
+      const f32x4 v = *reinterpret_cast<const f32x4*>(po + (size_t)s * dh);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) r[e] += v[e] * f;
+    }
   }
-  if (lane == 0 && a.lse) a.lse[col_id] = sum == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * LN2;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) xs[g8][4 * i + e] = r[e];
+  if (i == 0) xs[g8][128] = sum;
+  __syncthreads();
+  sum = 0.f;
+#pragma unroll
+  for (int v = 0; v < 8; ++v) sum += xs[v][128];
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  if (threadIdx.x < dh) {
+    float o = 0.f;
+#pragma unroll
+    for (int v = 0; v < 8; ++v) o += xs[v][threadIdx.x];
+    static_cast<T*>(a.o)[(((size_t)b * L + j) * a.p.Hkv * a.G + h * a.G + g) * dh + threadIdx.x] = from_f32<T>(o * inv);
+  }
+  if (threadIdx.x == 0 && a.lse) a.lse[col_id] = sum == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * LN2;
 }
 
 struct Plan {
@@ -360,8 +385,7 @@ hipError_t launch(const Args& a, const Plan& pl, hipStream_t s) {
   else
     launch_timed(attend_kernel<T, NB, 1>, dim3((unsigned)blocks), dim3(64 * NW), 0, s, a);
   if (pl.S > 1) {
-    const long cols = (long)a.r.B * a.p.Hkv * ncol;
-    hipLaunchKernelGGL(join_kernel<T>, dim3((unsigned)((cols + 3) / 4)), dim3(256), 0, s, a);
+    hipLaunchKernelGGL(join_kernel<T>, dim3((unsigned)(a.r.B * a.p.Hkv * ncol)), dim3(256), 0, s, a);
   }
   return hipGetLastError();
 }
