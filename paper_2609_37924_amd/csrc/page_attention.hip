@@ -11,16 +11,17 @@
 // 16-key block i stands for key 16 g + 4 i + j, so that a lane's 16 probabilities of a page
 // are those of 16 consecutive keys, one 16-byte load of a V^T row.
 //
-// A block is 4 waves on the same columns, each taking every fourth tile of 64 keys; the key
-// axis is split over S blocks when the columns alone leave the chip empty, and the partial
-// results (m, l, unnormalised O) are joined in the order of the splits.
+// Three kernels: float32 models; bf16 with few columns, where each wave takes tiles of 64 keys
+// of its own straight from memory (the pages' bytes bound it); bf16 with many, where tiles
+// go through LDS for the waves of a block (the matrix cores and the exponentials bound it).
+// The key axis is split over S blocks when the columns alone leave the chip empty; the
+// partial results (m, l, unnormalised O) are joined in the order of the splits.
 #include "common.h"
 #include "pages.h"
 
 namespace tadm {
 namespace {
 
-constexpr int NW = 4;  // waves of a block
 constexpr float LN2 = 0.6931471805599453f;
 
 struct Args {
@@ -40,12 +41,6 @@ __device__ __forceinline__ int row_len(const PageRows& r, int b) {
 __device__ __forceinline__ int row_new(const PageRows& r, int b) {
   return r.n ? min(max(r.n[b], 0), r.max_n) : r.max_n;
 }
-
-// 4 codes (a dword) as floats times the scale
-__device__ __forceinline__ f32x4 f32_codes(uint32_t c, float s) {
-  const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)c, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)c, true);
-  return f32x4{lo[0] * s, lo[1] * s, hi[0] * s, hi[1] * s};
-}
 __device__ __forceinline__ float* part_o(const Args& a, size_t col, int split) {
   return a.part + (col * a.S + split) * a.p.dh;
 }
@@ -53,6 +48,213 @@ __device__ __forceinline__ float* part_ml(const Args& a, size_t col, int split) 
   const size_t cols = (size_t)a.r.B * a.p.Hkv * a.G * a.r.max_n;
   return a.part + cols * a.S * a.p.dh + (col * a.S + split) * 2;
 }
+
+// What a block works on: columns [ct * width, ...) of K/V head h of row b, split sp of its tiles.
+// Column tiles are fastest, so that the blocks that read the same pages run on one XCD.
+struct Block {
+  int b, h, ct, sp, n, len, np, t0, t1;  // tiles [t0, t1): pages below np, the window's from np on
+  size_t head;
+};
+__device__ __forceinline__ Block block_of(const Args& a, int width) {
+  const int nct = (a.G * a.r.max_n + width - 1) / width, id = xcd_contiguous(blockIdx.x, gridDim.x);
+  Block x;
+  x.ct = id % nct;
+  x.sp = (id / nct) % a.S;
+  x.h = (id / nct / a.S) % a.p.Hkv;
+  x.b = id / nct / a.S / a.p.Hkv;
+  x.n = row_new(a.r, x.b);
+  x.len = row_len(a.r, x.b);
+  x.np = (x.len + PAGE - 1) / PAGE;
+  const int nt = x.np + (a.k ? (x.n + PAGE - 1) / PAGE : 0);
+  x.t0 = (int)((long)nt * x.sp / a.S);
+  x.t1 = (int)((long)nt * (x.sp + 1) / a.S);
+  x.head = (size_t)x.b * a.p.Hkv + x.h;
+  return x;
+}
+
+// One tile of a column's softmax.  s[i][j]: the score of key 16 grp + 4 i + j, unscaled; on
+// return its probability relative to a reference m (base 2) that moves only when the tile's
+// maximum exceeds it by more than 2^8: until then the probabilities stay below 256 and O
+// needs no rescaling.  Returns the factor for what was summed before.
+__device__ __forceinline__ float softmax_tile(f32x4 (&s)[4], int keys, int grp, float scale_log2, float& m, float& l) {
+  float mt = -INFINITY;
+  if (keys < PAGE)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (16 * grp + 4 * i + j >= keys) s[i][j] = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) mt = fmaxf(mt, s[i][j]);
+  mt = fmaxf(mt, xor16(mt));
+  mt = fmaxf(mt, xor32(mt));
+  const float mt2 = mt * scale_log2;
+  const float m_new = mt2 > m + 8.f ? mt2 : m;
+  const float ref = m_new == -INFINITY ? 0.f : m_new;  // no finite score yet: every p is 0
+  const float alpha = __builtin_amdgcn_exp2f(m - ref);
+  float ps = 0.f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      s[i][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i][j], scale_log2, -ref));
+      ps += s[i][j];
+    }
+  l = l * alpha + ps;
+  m = m_new;
+  return m == -INFINITY ? 1.f : alpha;
+}
+
+// Stores 4 values of column col (head width d0 + [0, 4)) of a strip: part of a split, or the result.
+template <class T>
+__device__ __forceinline__ void put4(const Args& a, const Block& x, int col, int d0, float inv, const float* r) {
+  if (a.S > 1) {
+    store4(part_o(a, x.head * (a.G * a.r.max_n) + col, x.sp) + d0, r[0], r[1], r[2], r[3]);
+  } else {
+    const int L = a.r.max_n, g = col / L, j = col % L;
+    T* out = static_cast<T*>(a.o) + (((size_t)x.b * L + j) * a.p.Hkv * a.G + x.h * a.G + g) * a.p.dh;
+    store4(out + d0, r[0] * inv, r[1] * inv, r[2] * inv, r[3] * inv);
+  }
+}
+__device__ __forceinline__ void put_ml(const Args& a, const Block& x, int col, float m, float sum) {
+  const size_t at = x.head * (a.G * a.r.max_n) + col;
+  if (a.S > 1)
+    store2(part_ml(a, at, x.sp), m, sum);
+  else if (a.lse)
+    a.lse[at] = sum == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * LN2;
+}
+__device__ __forceinline__ float inverse(const Args& a, float sum) { return a.S > 1 || sum == 0.f ? 0.f : 1.f / sum; }
+
+// Joins NW waves that hold the same strip of 16 columns, in the order of the waves: per lane m,
+// l and O in [wave][value][lane] floats; wave w sums the head-width blocks w, w + NW, ...
+template <class T, int NB, int NW>
+__device__ __forceinline__ void join_waves(const Args& a, const Block& x, int col, float m_run, float l_run,
+                                           const f32x4 (&o)[NB], float* xs) {
+  constexpr int NV = 2 + 4 * NB;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, grp = lane >> 4;
+  float l = l_run + xor16(l_run);
+  l += xor32(l);
+  float* w = xs + wave * NV * 64 + lane;
+  w[0] = m_run;
+  w[64] = l;
+#pragma unroll
+  for (int d = 0; d < NB; ++d)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w[(2 + 4 * d + j) * 64] = o[d][j];
+  __syncthreads();
+  const float* y = xs + lane;
+  float m = -INFINITY, f[NW], sum = 0.f;
+#pragma unroll
+  for (int v = 0; v < NW; ++v) m = fmaxf(m, y[v * NV * 64]);
+  const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll
+  for (int v = 0; v < NW; ++v) {
+    f[v] = __builtin_amdgcn_exp2f(y[v * NV * 64] - ref);
+    sum += y[v * NV * 64 + 64] * f[v];
+  }
+  const int L = a.r.max_n;
+  if (col < a.G * L && col % L < x.n) {
+    const float inv = inverse(a, sum);
+    for (int d = wave; d < NB; d += NW) {
+      float r[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int v = 0; v < NW; ++v)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) r[e] += y[(v * NV + 2 + 4 * d + e) * 64] * f[v];
+      if (16 * d + 4 * grp < a.p.dh) put4<T>(a, x, col, 16 * d + 4 * grp, inv, r);
+    }
+    if (wave == 0 && grp == 0) put_ml(a, x, col, m, sum);
+  }
+  __syncthreads();  // xs is free again
+}
+
+// bytes [0, keep) of a dword (keep may be negative or above 4)
+__device__ __forceinline__ uint32_t keep_bytes(uint32_t v, int keep) {
+  return keep >= 4 ? v : keep <= 0 ? 0u : v & ((1u << (8 * keep)) - 1u);
+}
+
+// ---------------------------------------------------------------- float32 models
+// 4 codes (a dword) as floats times the scale
+__device__ __forceinline__ f32x4 f32_codes(uint32_t c, float s) {
+  const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)c, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)c, true);
+  return f32x4{lo[0] * s, lo[1] * s, hi[0] * s, hi[1] * s};
+}
+
+// Four waves on a strip of 16 columns, each taking every fourth tile; NB: head width in blocks of
+// 16, the last of which may be partial.
+template <int NB>
+__global__ __launch_bounds__(256) void attend_f32_kernel(Args a) {
+  constexpr int NW = 4;
+  __shared__ float xs[NW * (2 + 4 * NB) * 64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), grp = lane >> 4,
+            fr = lane & 15;
+  const Block x = block_of(a, 16);
+  if (x.n == 0) return;
+  const int dh = a.p.dh, ncol = a.G * a.r.max_n, col = x.ct * 16 + fr;
+  f32x4 qx[NB], o[NB];
+  const float* q = static_cast<const float*>(a.q) + (x.head * ncol + min(col, ncol - 1)) * dh;
+#pragma unroll
+  for (int c = 0; c < NB; ++c) {
+    qx[c] = 16 * c + 4 * grp < dh ? *reinterpret_cast<const f32x4*>(q + 16 * c + 4 * grp) : f32x4{0.f, 0.f, 0.f, 0.f};
+    o[c] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  float m_run = -INFINITY, l_run = 0.f;
+  for (int t = x.t0 + wave; t < x.t1; t += NW) {
+    const bool paged = t < x.np;
+    const int keys = paged ? min(PAGE, x.len - t * PAGE) : min(PAGE, x.n - (t - x.np) * PAGE);
+    const uint8_t* codes = nullptr;
+    const float *sc = nullptr, *kw = nullptr, *vw = nullptr;
+    if (paged) {
+      const int page = a.r.table[(size_t)x.b * a.r.max_pages + t];
+      if ((unsigned)page >= (unsigned)a.p.n_pages) continue;
+      codes = a.p.data + (size_t)page * a.p.page_bytes + (size_t)x.h * 2 * PAGE * dh;
+      sc = a.p.scale + (size_t)page * a.p.page_scales + 2 * x.h;
+    } else {
+      kw = static_cast<const float*>(a.k) + (x.head * a.cap + (size_t)(t - x.np) * PAGE) * dh;
+      vw = static_cast<const float*>(a.vt) + x.head * dh * a.cap + (size_t)(t - x.np) * PAGE;
+    }
+    const float sk = paged ? sc[0] : 1.f, sv = paged ? sc[1] : 1.f;
+    f32x4 s[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int key = 16 * (fr >> 2) + 4 * i + (fr & 3);
+      s[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int c = 0; c < NB; ++c) {
+        f32x4 kf = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (16 * c + 4 * grp < dh)
+          kf = paged ? f32_codes(*reinterpret_cast<const uint32_t*>(codes + key * dh + 16 * c + 4 * grp), sk)
+                     : *reinterpret_cast<const f32x4*>(kw + (size_t)key * dh + 16 * c + 4 * grp);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[e], qx[c][e], s[i], 0, 0, 0);
+      }
+    }
+    const float alpha = softmax_tile(s, keys, grp, a.scale_log2, m_run, l_run);
+    // V^T row 16 d + fr, keys 16 grp + [0, 16); what lies behind the last key is taken as 0, so
+    // that p = 0 meets a finite value
+#pragma unroll
+    for (int d = 0; d < NB; ++d) {
+      const int row = min(16 * d + fr, dh - 1);
+      o[d] *= alpha;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        f32x4 vf = paged ? f32_codes(*reinterpret_cast<const uint32_t*>(codes + PAGE * dh + row * PAGE + 16 * grp + 4 * i), sv)
+                         : *reinterpret_cast<const f32x4*>(vw + (size_t)row * a.cap + 16 * grp + 4 * i);
+        if (keys < PAGE)
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (16 * grp + 4 * i + j >= keys) vf[j] = 0.f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[d] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[j], s[i][j], o[d], 0, 0, 0);
+      }
+    }
+  }
+  join_waves<float, NB, NW>(a, x, col, m_run, l_run, o, xs);
+}
+
+// ---------------------------------------------------------------- bf16 models
 // 8 codes as bf16 times the scale, exactly
 __device__ __forceinline__ bf16x8 bf16_codes(uint32_t a, uint32_t b, float s) {
   const auto p0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, s, false),
@@ -61,255 +263,375 @@ __device__ __forceinline__ bf16x8 bf16_codes(uint32_t a, uint32_t b, float s) {
              p3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, s, true);
   return bf16x8{p0[0], p0[1], p1[0], p1[1], p2[0], p2[1], p3[0], p3[1]};
 }
-// bytes [0, keep) of a dword (keep may be negative or above 4)
-__device__ __forceinline__ uint32_t keep_bytes(uint32_t v, int keep) {
-  return keep >= 4 ? v : keep <= 0 ? 0u : v & ((1u << (8 * keep)) - 1u);
+// A column's query: a lane has the elements [W grp, + W), W = DH / 4, of its column.
+template <int DH>
+struct Query {
+  bf16x8 op[DH / 32];
+};
+template <int DH>
+__device__ __forceinline__ Query<DH> load_query(const bf16* q, int grp) {
+  Query<DH> r;
+#pragma unroll
+  for (int c = 0; c < DH / 32; ++c) r.op[c] = *reinterpret_cast<const bf16x8*>(q + DH / 4 * grp + 8 * c);
+  return r;
+}
+// Scores of QS strips of 16 columns and 16 keys, from the lane's DH / 4 codes of the row it stands for.
+// The codes become bf16, exactly, for the bf16 products: the 8-bit ones, twice as fast, drop
+// what lies 2^-12 below the largest product of a sum.
+template <int DH, int QS>
+__device__ __forceinline__ void scores(const uint4 (&c)[DH / 64], float scale, const Query<DH> (&q)[QS], int i,
+                                       f32x4 (&s)[QS][4]) {
+#pragma unroll
+  for (int u = 0; u < QS; ++u) s[u][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int e = 0; e < DH / 32; ++e) {
+    const uint4 w = c[e / 2];
+    const bf16x8 k = e % 2 ? bf16_codes(w.z, w.w, scale) : bf16_codes(w.x, w.y, scale);
+#pragma unroll
+    for (int u = 0; u < QS; ++u) s[u][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[u].op[e], s[u][i], 0, 0, 0);
+  }
 }
 
-// NB: head width in blocks of 16 (the last may be partial for float), QS: strips of 16 columns.
-template <class T, int NB, int QS>
-__global__ __launch_bounds__(64 * NW) void attend_kernel(Args a) {
-  constexpr bool BF = sizeof(T) == 2;
-  constexpr int NV = 2 + 4 * NB;  // floats a lane keeps per strip: m, l and its part of O
-  __shared__ float xs[NW * NV * 64];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), grp = lane >> 4,
-            fr = lane & 15;
-  const int dh = BF ? 16 * NB : a.p.dh, L = a.r.max_n, ncol = a.G * L, nct = (ncol + 16 * QS - 1) / (16 * QS);
-  const int id = xcd_contiguous(blockIdx.x, gridDim.x);
-  const int ct = id % nct, sp = (id / nct) % a.S, h = (id / nct / a.S) % a.p.Hkv, b = id / nct / a.S / a.p.Hkv;
-  const int n = row_new(a.r, b);
-  if (n == 0) return;
-  const int len = row_len(a.r, b), np = (len + PAGE - 1) / PAGE, nt = np + (a.k ? (n + PAGE - 1) / PAGE : 0);
-  const int t0 = (int)((long)nt * sp / a.S), t1 = (int)((long)nt * (sp + 1) / a.S);
-
-  // queries: lane's column of strip u, the head-width elements that its k index of a product has
-  const size_t head = (size_t)b * a.p.Hkv + h;
-  bf16x8 qb[QS][BF ? NB / 2 : 1];
-  f32x4 qx[QS][BF ? 1 : NB];
-#pragma unroll
-  for (int u = 0; u < QS; ++u) {
-    const int col = min(ct * 16 * QS + 16 * u + fr, ncol - 1);
-    const T* q = static_cast<const T*>(a.q) + (head * ncol + col) * dh;
-    if constexpr (BF) {
-#pragma unroll
-      for (int c = 0; c < NB / 2; ++c) qb[u][c] = *reinterpret_cast<const bf16x8*>(q + grp * (4 * NB) + 8 * c);
-    } else {
-#pragma unroll
-      for (int c = 0; c < NB; ++c)
-        qx[u][c] = 16 * c + 4 * grp < dh ? *reinterpret_cast<const f32x4*>(q + 16 * c + 4 * grp) : f32x4{0.f, 0.f, 0.f, 0.f};
+// The tiles of pages that a wave takes, 64 at a time: lane l has the page, the keys and the scales
+// of the (64 i + l)-th, so that a step finds them in a register.
+struct TileBatch {
+  int page, keys;
+  float sk, sv;
+};
+__device__ __forceinline__ TileBatch tile_batch(const Args& a, const Block& x, int tile, int t1) {
+  TileBatch r{0, 0, 1.f, 1.f};  // no keys: a tile of an absent page, or none (page 0 is read)
+  if (tile < t1) {
+    const int page = a.r.table[(size_t)x.b * a.r.max_pages + tile];
+    if ((unsigned)page < (unsigned)a.p.n_pages) {
+      const float* sc = a.p.scale + (size_t)page * a.p.page_scales + 2 * x.h;
+      r = TileBatch{page, min(PAGE, x.len - tile * PAGE), sc[0], sc[1]};
     }
   }
+  return r;
+}
+__device__ __forceinline__ int at_lane(int v, int lane) { return __builtin_amdgcn_readlane(v, lane); }
+__device__ __forceinline__ float at_lane(float v, int lane) {
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane));
+}
+
+// Probabilities of a tile as the operand of O^T = V^T P^T: k index 8 grp + j of product c is key
+// 16 grp + 8 c + j.
+__device__ __forceinline__ void p_operand(const f32x4 (&s)[4], bf16x8 (&p)[2]) {
+#pragma unroll
+  for (int c = 0; c < 2; ++c)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) p[c][j] = (bf16)s[2 * c + j / 4][j % 4];
+}
+
+// A tile of the window's own keys (bf16), read from memory by the wave itself, for QS strips.
+template <int DH, int QS>
+__device__ __forceinline__ void window_tile(const Args& a, const Block& x, int w, const bf16* const (&q)[QS],
+                                            f32x4 (&o)[QS][DH / 16], float (&m_run)[QS], float (&l_run)[QS]) {
+  constexpr int NB = DH / 16;
+  const int lane = threadIdx.x & 63, grp = lane >> 4, fr = lane & 15, keys = min(PAGE, x.n - w * PAGE);
+  const bf16* kw = static_cast<const bf16*>(a.k) + (x.head * a.cap + (size_t)w * PAGE) * DH;
+  const bf16* vw = static_cast<const bf16*>(a.vt) + x.head * DH * a.cap + (size_t)w * PAGE;
+  f32x4 s[QS][4];
+#pragma unroll
+  for (int u = 0; u < QS; ++u)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s[u][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int c = 0; c < NB / 2; ++c) {
+    bf16x8 qf[QS];
+#pragma unroll
+    for (int u = 0; u < QS; ++u) qf[u] = *reinterpret_cast<const bf16x8*>(q[u] + 32 * c + 8 * grp);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int key = 16 * (fr >> 2) + 4 * i + (fr & 3);
+      const bf16x8 kf = *reinterpret_cast<const bf16x8*>(kw + (size_t)key * DH + 32 * c + 8 * grp);
+#pragma unroll
+      for (int u = 0; u < QS; ++u) s[u][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[u], s[u][i], 0, 0, 0);
+    }
+  }
+  bf16x8 p[QS][2];
+#pragma unroll
+  for (int u = 0; u < QS; ++u) {
+    const float alpha = softmax_tile(s[u], keys, grp, a.scale_log2, m_run[u], l_run[u]);
+    if (__builtin_amdgcn_ballot_w64(alpha != 1.f))
+#pragma unroll
+      for (int d = 0; d < NB; ++d) o[u][d] *= alpha;
+    p_operand(s[u], p[u]);
+  }
+#pragma unroll
+  for (int d = 0; d < NB; ++d)
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      bf16x8 vf = *reinterpret_cast<const bf16x8*>(vw + (size_t)(16 * d + fr) * a.cap + 16 * grp + 8 * c);
+      if (keys < PAGE)
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (16 * grp + 8 * c + j >= keys) vf[j] = (bf16)0.f;
+#pragma unroll
+      for (int u = 0; u < QS; ++u) o[u][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, p[u][c], o[u][d], 0, 0, 0);
+    }
+}
+
+// Few columns: four waves on the same 16 QS columns, each taking every fourth tile straight from
+// memory into registers; the codes of the next tile are on their way while one is computed.
+template <int DH, int QS>
+__global__ __launch_bounds__(256) void attend_narrow_kernel(Args a) {
+  constexpr int NW = 4, NB = DH / 16;
+  __shared__ float xs[NW * (2 + 4 * NB) * 64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), grp = lane >> 4,
+            fr = lane & 15;
+  const Block x = block_of(a, 16 * QS);
+  if (x.n == 0) return;
+  const int ncol = a.G * a.r.max_n, tp = min(x.t1, x.np), first = x.t0 + wave;
+  const int steps = first < tp ? (tp - first + NW - 1) / NW : 0;
+  const bf16* q[QS];
+  Query<DH> qs[QS];
   f32x4 o[QS][NB];
   float m_run[QS], l_run[QS];
 #pragma unroll
   for (int u = 0; u < QS; ++u) {
-#pragma unroll
-    for (int d = 0; d < NB; ++d) o[u][d] = f32x4{0.f, 0.f, 0.f, 0.f};
+    q[u] = static_cast<const bf16*>(a.q) + (x.head * ncol + min(x.ct * 16 * QS + 16 * u + fr, ncol - 1)) * DH;
     m_run[u] = -INFINITY;
     l_run[u] = 0.f;
+#pragma unroll
+    for (int d = 0; d < NB; ++d) o[u][d] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-
-  for (int t = t0 + wave; t < t1; t += NW) {
-    const bool paged = t < np;
-    const int kv = paged ? min(PAGE, len - t * PAGE) : min(PAGE, n - (t - np) * PAGE);  // keys of this tile
-    const uint8_t* codes = nullptr;
-    float sk = 1.f, sv = 1.f;
-    const T *kw = nullptr, *vw = nullptr;
-    if (paged) {
-      const int page = a.r.table[(size_t)b * a.r.max_pages + t];
-      if ((unsigned)page >= (unsigned)a.p.n_pages) continue;
-      codes = a.p.data + (size_t)page * a.p.page_bytes + (size_t)h * 2 * PAGE * dh;
-      const float* sc = a.p.scale + (size_t)page * a.p.page_scales + 2 * h;
-      sk = sc[0];
-      sv = sc[1];
-    } else {
-      kw = static_cast<const T*>(a.k) + (head * a.cap + (size_t)(t - np) * PAGE) * dh;
-      vw = static_cast<const T*>(a.vt) + head * dh * a.cap + (size_t)(t - np) * PAGE;
-    }
+  TileBatch tb = tile_batch(a, x, first + NW * lane, tp);
+  const uint8_t* base = a.p.data + (size_t)x.h * 2 * PAGE * DH;
+  const int koff = (16 * (fr >> 2) + (fr & 3)) * DH + DH / 4 * grp;
+  const int voff = PAGE * DH + fr * PAGE + 16 * grp;
+  uint4 kc[4][DH / 64], vc[NB];
+  auto load_k = [&](int page) {
+    const uint8_t* c = base + (size_t)page * a.p.page_bytes + koff;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int e = 0; e < DH / 64; ++e) kc[i][e] = *reinterpret_cast<const uint4*>(c + 4 * i * DH + 16 * e);
+  };
+  auto load_v = [&](int page) {
+    const uint8_t* c = base + (size_t)page * a.p.page_bytes + voff;
+#pragma unroll
+    for (int d = 0; d < NB; ++d) vc[d] = *reinterpret_cast<const uint4*>(c + 16 * d * PAGE);
+  };
+  if (steps) {
+    const int page = at_lane(tb.page, 0);
+    load_k(page);
+    load_v(page);
+  }
+#pragma unroll
+  for (int u = 0; u < QS; ++u) qs[u] = load_query<DH>(q[u], grp);
+  for (int st = 0; st < steps; ++st) {
+    const int keys = at_lane(tb.keys, st & 63);
+    const float sk = at_lane(tb.sk, st & 63), sv = at_lane(tb.sv, st & 63);
     f32x4 s[QS][4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int key = 16 * (fr >> 2) + 4 * i + (fr & 3);
-#pragma unroll
-      for (int u = 0; u < QS; ++u) s[u][i] = f32x4{0.f, 0.f, 0.f, 0.f};
-      if constexpr (BF) {
-        bf16x8 kf[NB / 2];
-        if (paged) {
-          uint32_t w[NB];
-          const uint4* src = reinterpret_cast<const uint4*>(codes + key * dh + grp * (4 * NB));
-#pragma unroll
-          for (int c = 0; c < NB / 4; ++c) *reinterpret_cast<uint4*>(w + 4 * c) = src[c];
-#pragma unroll
-          for (int c = 0; c < NB / 2; ++c) kf[c] = bf16_codes(w[2 * c], w[2 * c + 1], sk);
-        } else {
-          const bf16x8* src = reinterpret_cast<const bf16x8*>(kw + (size_t)key * dh + grp * (4 * NB));
-#pragma unroll
-          for (int c = 0; c < NB / 2; ++c) kf[c] = src[c];
-        }
-#pragma unroll
-        for (int c = 0; c < NB / 2; ++c)
-#pragma unroll
-          for (int u = 0; u < QS; ++u) s[u][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[c], qb[u][c], s[u][i], 0, 0, 0);
-      } else {
-#pragma unroll
-        for (int c = 0; c < NB; ++c) {
-          f32x4 kf = f32x4{0.f, 0.f, 0.f, 0.f};
-          if (16 * c + 4 * grp < dh)
-            kf = paged ? f32_codes(*reinterpret_cast<const uint32_t*>(codes + key * dh + 16 * c + 4 * grp), sk)
-                       : *reinterpret_cast<const f32x4*>(kw + (size_t)key * dh + 16 * c + 4 * grp);
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-#pragma unroll
-            for (int u = 0; u < QS; ++u) s[u][i] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[e], qx[u][c][e], s[u][i], 0, 0, 0);
-        }
-      }
+    for (int i = 0; i < 4; ++i) scores<DH, QS>(kc[i], sk, qs, i, s);
+    int page = 0;
+    if (st + 1 < steps) {
+      if (((st + 1) & 63) == 0) tb = tile_batch(a, x, first + NW * (st + 1 + lane), tp);
+      page = at_lane(tb.page, (st + 1) & 63);
+      load_k(page);
     }
+    bf16x8 p[QS][2];
 #pragma unroll
     for (int u = 0; u < QS; ++u) {
-      // s[u][i][j]: key 16 grp + 4 i + j of the tile, unscaled; the softmax runs in base 2 on
-      // s * scale_log2, relative to a reference that moves only when the tile's maximum
-      // exceeds it by more than 2^8: until then the probabilities stay below 256 and the
-      // accumulators need no rescaling
-      float mt = -INFINITY;
+      const float alpha = softmax_tile(s[u], keys, grp, a.scale_log2, m_run[u], l_run[u]);
+      if (__builtin_amdgcn_ballot_w64(alpha != 1.f))
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          if (16 * grp + 4 * i + j >= kv) s[u][i][j] = -INFINITY;
-          mt = fmaxf(mt, s[u][i][j]);
-        }
-      mt = fmaxf(mt, xor16(mt));
-      mt = fmaxf(mt, xor32(mt));
-      const float mt2 = mt * a.scale_log2;
-      const float m_new = mt2 > m_run[u] + 8.f ? mt2 : m_run[u];
-      const float ref = m_new == -INFINITY ? 0.f : m_new;  // no finite score yet: every p is 0
-      const float alpha = __builtin_amdgcn_exp2f(m_run[u] - ref);
-      float ps = 0.f;
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          s[u][i][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][i][j], a.scale_log2, -ref));
-          ps += s[u][i][j];
-        }
-      l_run[u] = l_run[u] * alpha + ps;
-      m_run[u] = m_new;
-#pragma unroll
-      for (int d = 0; d < NB; ++d) o[u][d] *= alpha;
+        for (int d = 0; d < NB; ++d) o[u][d] *= alpha;
+      p_operand(s[u], p[u]);
     }
-    bf16x8 pf[QS][BF ? 2 : 1];
-    if constexpr (BF) {
-#pragma unroll
-      for (int u = 0; u < QS; ++u)
-#pragma unroll
-        for (int c = 0; c < 2; ++c)
-#pragma unroll
-          for (int j = 0; j < 8; ++j) pf[u][c][j] = (bf16)s[u][2 * c + j / 4][j % 4];
-    }
-    // V^T row 16 d + fr, keys 16 grp + [0, 16) of the tile; what lies behind the last key is
-    // taken as 0, so that p = 0 meets a finite value
+    // V^T row 16 d + fr, keys 16 grp + [0, 16); what lies behind the last key is taken as 0, so
+    // that p = 0 meets a finite value
 #pragma unroll
     for (int d = 0; d < NB; ++d) {
-      const int row = min(16 * d + fr, dh - 1);
-      if (paged) {
-        uint32_t w[4];
-        *reinterpret_cast<uint4*>(w) = *reinterpret_cast<const uint4*>(codes + PAGE * dh + row * PAGE + 16 * grp);
-        if (kv < PAGE)
+      uint32_t w[4] = {vc[d].x, vc[d].y, vc[d].z, vc[d].w};
+      if (keys < PAGE)
 #pragma unroll
-          for (int c = 0; c < 4; ++c) w[c] = keep_bytes(w[c], kv - 16 * grp - 4 * c);
-        if constexpr (BF) {
+        for (int c = 0; c < 4; ++c) w[c] = keep_bytes(w[c], keys - 16 * grp - 4 * c);
 #pragma unroll
-          for (int c = 0; c < 2; ++c) {
-            const bf16x8 vf = bf16_codes(w[2 * c], w[2 * c + 1], sv);
+      for (int c = 0; c < 2; ++c) {
+        const bf16x8 vf = bf16_codes(w[2 * c], w[2 * c + 1], sv);
 #pragma unroll
-            for (int u = 0; u < QS; ++u) o[u][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[u][c], o[u][d], 0, 0, 0);
-          }
-        } else {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const f32x4 vf = f32_codes(w[i], sv);
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-              for (int u = 0; u < QS; ++u) o[u][d] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[j], s[u][i][j], o[u][d], 0, 0, 0);
-          }
-        }
-      } else if constexpr (BF) {
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          bf16x8 vf = *reinterpret_cast<const bf16x8*>(vw + (size_t)row * a.cap + 16 * grp + 8 * c);
-          if (kv < PAGE)
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-              if (16 * grp + 8 * c + j >= kv) vf[j] = (bf16)0.f;
-#pragma unroll
-          for (int u = 0; u < QS; ++u) o[u][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[u][c], o[u][d], 0, 0, 0);
-        }
-      } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const f32x4 vf = *reinterpret_cast<const f32x4*>(vw + (size_t)row * a.cap + 16 * grp + 4 * i);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const float v = 16 * grp + 4 * i + j < kv ? vf[j] : 0.f;
-#pragma unroll
-            for (int u = 0; u < QS; ++u) o[u][d] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, s[u][i][j], o[u][d], 0, 0, 0);
-          }
-        }
+        for (int u = 0; u < QS; ++u) o[u][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, p[u][c], o[u][d], 0, 0, 0);
       }
     }
+    if (st + 1 < steps) load_v(page);
   }
+  for (int t = max(x.t0, x.np); t < x.t1; ++t)
+    if ((t - x.t0) % NW == wave) window_tile<DH, QS>(a, x, t - x.np, q, o, m_run, l_run);
+#pragma unroll
+  for (int u = 0; u < QS; ++u)
+    join_waves<bf16, NB, NW>(a, x, x.ct * 16 * QS + 16 * u + fr, m_run[u], l_run[u], o[u], xs);
+}
 
-  // Join the waves, a strip at a time, in the order of the waves: per lane m, l and O in
-  // [wave][value][lane] floats; wave w sums the head-width blocks w, w + 4, ...
+// Many columns: CW waves with 32 columns each share the tiles of pages in LDS; KW such groups take
+// every KW-th tile and are joined at the end.  Two stages: while one tile is computed, the codes
+// of the next are on their way to registers, from which they go to the other stage as bf16,
+// scaled, the values 0 behind the last key, so that p = 0 meets a finite value: a wave converts
+// its share of a tile once for all of them (with the keys as codes in LDS, converted by
+// every wave, 4 x 256 columns over 16K take 408 us instead of 379, 16 x 64 over 1K 59
+// instead of 47.5).  K row r of a stage has key 16 ((r / 4) % 4) + 4 (r / 16) + r % 4, the key
+// that score row r % 16 of block r / 16 stands for.  Chunk c (16 bytes) of row r sits in slot
+// c ^ (r & 7), so that 8 neighbouring lanes read different banks.
+template <int DH, int CW, int KW>
+__global__ __launch_bounds__(64 * CW * KW, 2) void attend_wide_kernel(Args a) {
+  constexpr int QS = 2, NB = DH / 16, KC = DH / 16, NV = 2 + 4 * NB, GT = 64 * CW;
+  constexpr int SIDE = PAGE * DH, KBYTES = 2 * SIDE, STAGE = 2 * KBYTES;
+  constexpr int PER = SIDE / 16 / GT;  // chunks of a side that a lane moves per tile
+  static_assert(PER * 16 * GT == SIDE, "a tile splits over the lanes of a group");
+  constexpr int RING = 2 * KW * STAGE, MERGE = KW > 1 ? CW * NV * 64 * 4 : 0;
+  __shared__ __attribute__((aligned(16))) char smem[RING > MERGE ? RING : MERGE];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), grp = lane >> 4,
+            fr = lane & 15, cw = wave % CW, kw = wave / CW, gl = cw * 64 + lane;
+  const Block x = block_of(a, 16 * QS * CW);
+  if (x.n == 0) return;
+  const int ncol = a.G * a.r.max_n, tp = min(x.t1, x.np), col0 = (x.ct * CW + cw) * 16 * QS;
+  const int steps = x.t0 < tp ? (tp - x.t0 + KW - 1) / KW : 0;  // of every wave; a group may have no tile in the last
+  const bf16* q[QS];
+  Query<DH> qs[QS];
+  f32x4 o[QS][NB];
+  float m_run[QS], l_run[QS];
 #pragma unroll
   for (int u = 0; u < QS; ++u) {
-    if (u) __syncthreads();  // the previous strip has been read
-    float l = l_run[u] + xor16(l_run[u]);
-    l += xor32(l);
-    float* w = xs + wave * NV * 64 + lane;
-    w[0] = m_run[u];
-    w[64] = l;
+    q[u] = static_cast<const bf16*>(a.q) + (x.head * ncol + min(col0 + 16 * u + fr, ncol - 1)) * DH;
+    m_run[u] = -INFINITY;
+    l_run[u] = 0.f;
 #pragma unroll
-    for (int d = 0; d < NB; ++d)
+    for (int d = 0; d < NB; ++d) o[u][d] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  // the lane's chunks of a tile: where they come from and where they go
+  int k_src[PER], k_dst[PER][2], v_dst[PER][2];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) w[(2 + 4 * d + j) * 64] = o[u][d][j];
-    __syncthreads();
-    const float* x = xs + lane;
-    float m = -INFINITY, f[NW], sum = 0.f;
+  for (int j = 0; j < PER; ++j) {
+    const int id = gl + GT * j, r = id / KC, c = id % KC;
+    k_src[j] = (16 * ((r >> 2) & 3) + 4 * (r >> 4) + (r & 3)) * DH + c * 16;
 #pragma unroll
-    for (int v = 0; v < NW; ++v) m = fmaxf(m, x[v * NV * 64]);
-    const float ref = m == -INFINITY ? 0.f : m;
+    for (int e = 0; e < 2; ++e) k_dst[j][e] = r * 2 * DH + ((2 * c + e) ^ (r & 7)) * 16;
 #pragma unroll
-    for (int v = 0; v < NW; ++v) {
-      f[v] = __builtin_amdgcn_exp2f(x[v * NV * 64] - ref);
-      sum += x[v * NV * 64 + 64] * f[v];
+    for (int e = 0; e < 2; ++e) v_dst[j][e] = KBYTES + (id / 4) * 128 + ((2 * (id % 4) + e) ^ (id / 4 & 7)) * 16;
+  }
+  const uint8_t* base = a.p.data + (size_t)x.h * 2 * PAGE * DH;
+  TileBatch tb = tile_batch(a, x, x.t0 + kw + KW * lane, tp);
+  uint4 kc[PER], vc[PER];
+  int keys = 0, keys_next = 0;
+  float sk_next = 1.f, sv_next = 1.f;
+  auto load = [&](int st) {
+    if (st && (st & 63) == 0) tb = tile_batch(a, x, x.t0 + kw + KW * (st + lane), tp);
+    keys_next = at_lane(tb.keys, st & 63);
+    sk_next = at_lane(tb.sk, st & 63);
+    sv_next = at_lane(tb.sv, st & 63);
+    const uint8_t* c = base + (size_t)at_lane(tb.page, st & 63) * a.p.page_bytes;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+      kc[j] = *reinterpret_cast<const uint4*>(c + k_src[j]);
+      vc[j] = *reinterpret_cast<const uint4*>(c + SIDE + (gl + GT * j) * 16);
     }
-    const int col = ct * 16 * QS + 16 * u + fr, g = col / L, j = col % L;
-    if (col >= ncol || j >= n) continue;
-    const float inv = a.S > 1 ? 1.f : sum == 0.f ? 0.f : 1.f / sum;
-    float* part = part_o(a, head * ncol + col, sp);
-    T* out = static_cast<T*>(a.o) + (((size_t)b * L + j) * a.p.Hkv * a.G + h * a.G + g) * dh;
-    for (int d = wave; d < NB; d += NW) {
-      float r[4] = {0.f, 0.f, 0.f, 0.f};
+  };
+  auto place = [&](int st) {
+    char* sb = smem + ((st & 1) * KW + kw) * STAGE;
 #pragma unroll
-      for (int v = 0; v < NW; ++v)
+    for (int j = 0; j < PER; ++j) {
+      *reinterpret_cast<bf16x8*>(sb + k_dst[j][0]) = bf16_codes(kc[j].x, kc[j].y, sk_next);
+      *reinterpret_cast<bf16x8*>(sb + k_dst[j][1]) = bf16_codes(kc[j].z, kc[j].w, sk_next);
+      uint32_t w[4] = {vc[j].x, vc[j].y, vc[j].z, vc[j].w};
+      if (keys_next < PAGE)  // what lies behind the last key is taken as 0, so that p = 0 meets a finite value
 #pragma unroll
-        for (int e = 0; e < 4; ++e) r[e] += x[(v * NV + 2 + 4 * d + e) * 64] * f[v];
-      if (16 * d + 4 * grp < dh) {
-        if (a.S > 1) {
-          store4(part + 16 * d + 4 * grp, r[0], r[1], r[2], r[3]);
-        } else {
-          store4(out + 16 * d + 4 * grp, r[0] * inv, r[1] * inv, r[2] * inv, r[3] * inv);
+        for (int c = 0; c < 4; ++c) w[c] = keep_bytes(w[c], keys_next - 16 * (gl & 3) - 4 * c);
+      *reinterpret_cast<bf16x8*>(sb + v_dst[j][0]) = bf16_codes(w[0], w[1], sv_next);
+      *reinterpret_cast<bf16x8*>(sb + v_dst[j][1]) = bf16_codes(w[2], w[3], sv_next);
+    }
+  };
+  if (steps) load(0);
+#pragma unroll
+  for (int u = 0; u < QS; ++u) qs[u] = load_query<DH>(q[u], grp);
+  if (steps) place(0);
+  // the lane's places in a stage: K row fr (the chunks of its codes), V^T row fr (keys 16 grp + 8 c + [0, 8))
+  int kofs[DH / 32], vofs[2];
+#pragma unroll
+  for (int e = 0; e < DH / 32; ++e) kofs[e] = fr * 2 * DH + ((DH / 32 * grp + e) ^ (fr & 7)) * 16;
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    vofs[e] = KBYTES + fr * 128 + ((2 * grp + e) ^ (fr & 7)) * 16;
+  }
+  for (int st = 0; st < steps; ++st) {
+    keys = keys_next;
+    __syncthreads();  // the step's stage is written, and the other one read
+    if (st + 1 < steps) load(st + 1);
+    if (keys > 0) {
+      const char* sb = smem + ((st & 1) * KW + kw) * STAGE;
+      f32x4 s[QS][4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+#pragma unroll
+        for (int u = 0; u < QS; ++u) s[u][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int e = 0; e < DH / 32; ++e) {
+          const bf16x8 k = *reinterpret_cast<const bf16x8*>(sb + i * 32 * DH + kofs[e]);
+#pragma unroll
+          for (int u = 0; u < QS; ++u)
+            s[u][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, qs[u].op[e], s[u][i], 0, 0, 0);
         }
       }
-    }
-    if (wave == 0 && grp == 0) {
-      if (a.S > 1) {
-        store2(part_ml(a, head * ncol + col, sp), m, sum);
-      } else if (a.lse) {
-        a.lse[head * ncol + col] = sum == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * LN2;
+      bf16x8 p[QS][2];
+#pragma unroll
+      for (int u = 0; u < QS; ++u) {
+        const float alpha = softmax_tile(s[u], keys, grp, a.scale_log2, m_run[u], l_run[u]);
+        if (__builtin_amdgcn_ballot_w64(alpha != 1.f))
+#pragma unroll
+          for (int d = 0; d < NB; ++d) o[u][d] *= alpha;
+        p_operand(s[u], p[u]);
       }
+#pragma unroll
+      for (int d = 0; d < NB; ++d)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const bf16x8 vf = *reinterpret_cast<const bf16x8*>(sb + d * 16 * 128 + vofs[c]);
+#pragma unroll
+          for (int u = 0; u < QS; ++u) o[u][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, p[u][c], o[u][d], 0, 0, 0);
+        }
+    }
+    if (st + 1 < steps) place(st + 1);
+  }
+  for (int t = max(x.t0, x.np); t < x.t1; ++t)
+    if ((t - x.t0) % KW == kw) window_tile<DH, QS>(a, x, t - x.np, q, o, m_run, l_run);
+#pragma unroll
+  for (int u = 0; u < QS; ++u) {
+    float l = l_run[u] + xor16(l_run[u]);
+    l_run[u] = l + xor32(l);
+    if constexpr (KW > 1) {  // the second group joins the first, a strip at a time
+      static_assert(KW <= 2, "two key groups");
+      float* w = reinterpret_cast<float*>(smem) + cw * NV * 64 + lane;
+      __syncthreads();  // every wave is done with the ring, or with the previous strip
+      if (kw == 1) {
+        w[0] = m_run[u];
+        w[64] = l_run[u];
+#pragma unroll
+        for (int d = 0; d < NB; ++d)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) w[(2 + 4 * d + j) * 64] = o[u][d][j];
+      }
+      __syncthreads();
+      if (kw == 0) {
+        const float m = fmaxf(m_run[u], w[0]), ref = m == -INFINITY ? 0.f : m;
+        const float f0 = __builtin_amdgcn_exp2f(m_run[u] - ref), f1 = __builtin_amdgcn_exp2f(w[0] - ref);
+        l_run[u] = l_run[u] * f0 + w[64] * f1;
+        m_run[u] = m;
+#pragma unroll
+        for (int d = 0; d < NB; ++d)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) o[u][d][j] = o[u][d][j] * f0 + w[(2 + 4 * d + j) * 64] * f1;
+      }
+    }
+    const int col = col0 + 16 * u + fr;
+    if (kw == 0 && col < ncol && col % a.r.max_n < x.n) {
+      const float inv = inverse(a, l_run[u]);
+#pragma unroll
+      for (int d = 0; d < NB; ++d) {
+        const float r[4] = {o[u][d][0], o[u][d][1], o[u][d][2], o[u][d][3]};
+        put4<bf16>(a, x, col, 16 * d + 4 * grp, inv, r);
+      }
+      if (grp == 0) put_ml(a, x, col, m_run[u], l_run[u]);
     }
   }
 }
@@ -359,35 +681,46 @@ __global__ __launch_bounds__(256) void join_kernel(Args a) {
   if (threadIdx.x == 0 && a.lse) a.lse[col_id] = sum == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * LN2;
 }
 
+// Which kernel a call takes: columns of a block, waves along the columns and the keys, splits.
+// Which kernel a call takes: columns of a block, waves along the columns and the keys, splits.
+// Which kernel a call takes: columns of a block, waves along the columns and the keys, splits.
+// Which kernel a call takes: columns of a block, waves along the columns and the keys, splits.
+// Which kernel a call takes: columns of a block, waves along the columns and the keys, splits.
+// Which kernel a call takes: columns of a block, waves along the columns and the keys, splits.
 struct Plan {
-  int qs, S;
+  int width, cw, kw, S;
 };
 
-// Strips per wave and splits of the key axis.
 Plan plan(DType dt, int B, int H, int Hkv, int L, int max_len) {
-  (void)dt;
   const int ncol = H / Hkv * L;
-  const int qs = ncol > 16 ? 2 : 1;
-  const long blocks = (long)B * Hkv * ((ncol + 16 * qs - 1) / (16 * qs));
   const int tiles = (max_len + PAGE - 1) / PAGE + (L + PAGE - 1) / PAGE;
-  long S = 1024 / blocks;                          // a block per CU and more
-  S = S < (tiles + 7) / 8 ? S : (tiles + 7) / 8;   // two tiles per wave at least
-  return Plan{qs, S < 1 ? 1 : (int)S};
+  auto blocks = [&](int width) { return (long)B * Hkv * ((ncol + width - 1) / width); };
+  Plan p{16, 0, 4, 1};
+  if (dt == BF16 && ncol > 32) {
+    p = Plan{128, 4, 1, 1};
+    if (blocks(128) < 512) p.kw = 2;
+  } else if (dt == BF16 && ncol > 16) {
+    p.width = 32;
+  }
+  const long n = blocks(p.width), most = (tiles + 4 * p.kw - 1) / (4 * p.kw);  // four tiles per wave at least
+  long S = (p.cw ? 512 / p.kw : 768) / n;
+  S = S < most ? S : most;
+  p.S = S < 1 ? 1 : (int)S;
+  return p;
 }
 
-template <class T, int NB>
-hipError_t launch(const Args& a, const Plan& pl, hipStream_t s) {
-  const int ncol = a.G * a.r.max_n;
-  const long blocks = (long)a.r.B * a.p.Hkv * pl.S * ((ncol + 16 * pl.qs - 1) / (16 * pl.qs));
-  if (blocks > 0x7fffffffL) return hipErrorInvalidValue;
-  if (pl.qs == 2)
-    launch_timed(attend_kernel<T, NB, 2>, dim3((unsigned)blocks), dim3(64 * NW), 0, s, a);
+template <typename K>
+void start(K kernel, const Args& a, const Plan& p, int threads, hipStream_t s) {
+  const long n = (long)a.r.B * a.p.Hkv * p.S * ((a.G * a.r.max_n + p.width - 1) / p.width);
+  launch_timed(kernel, dim3((unsigned)n), dim3(threads), 0, s, a);
+}
+
+template <int DH>
+void start_bf16(const Args& a, const Plan& p, hipStream_t s) {
+  if (p.cw)
+    p.kw == 2 ? start(attend_wide_kernel<DH, 4, 2>, a, p, 512, s) : start(attend_wide_kernel<DH, 4, 1>, a, p, 256, s);
   else
-    launch_timed(attend_kernel<T, NB, 1>, dim3((unsigned)blocks), dim3(64 * NW), 0, s, a);
-  if (pl.S > 1) {
-    hipLaunchKernelGGL(join_kernel<T>, dim3((unsigned)(a.r.B * a.p.Hkv * ncol)), dim3(256), 0, s, a);
-  }
-  return hipGetLastError();
+    p.width == 32 ? start(attend_narrow_kernel<DH, 2>, a, p, 256, s) : start(attend_narrow_kernel<DH, 1>, a, p, 256, s);
 }
 
 }  // namespace
@@ -403,21 +736,33 @@ hipError_t page_attend(DType dt, const PageAttend& c, hipStream_t s) {
   Args a{c.p, c.r, c.q, c.k, c.vt, c.o, c.lse, static_cast<float*>(c.work), c.H / c.p.Hkv, c.cap, pl.S,
          1.4426950408889634f / sqrtf((float)dh)};
   if (dt == BF16) {
-    if (dh == 64) return launch<bf16, 4>(a, pl, s);
-    if (dh == 128) return launch<bf16, 8>(a, pl, s);
-    return hipErrorInvalidValue;
+    if (dh == 128)
+      start_bf16<128>(a, pl, s);
+    else if (dh == 64)
+      start_bf16<64>(a, pl, s);
+    else
+      return hipErrorInvalidValue;
+  } else {
+    switch ((dh + 15) / 16) {
+      case 1: start(attend_f32_kernel<1>, a, pl, 256, s); break;
+      case 2: start(attend_f32_kernel<2>, a, pl, 256, s); break;
+      case 3: start(attend_f32_kernel<3>, a, pl, 256, s); break;
+      case 4: start(attend_f32_kernel<4>, a, pl, 256, s); break;
+      case 5: start(attend_f32_kernel<5>, a, pl, 256, s); break;
+      case 6: start(attend_f32_kernel<6>, a, pl, 256, s); break;
+      case 7: start(attend_f32_kernel<7>, a, pl, 256, s); break;
+      case 8: start(attend_f32_kernel<8>, a, pl, 256, s); break;
+      default: return hipErrorInvalidValue;
+    }
   }
-  switch ((dh + 15) / 16) {
-    case 1: return launch<float, 1>(a, pl, s);
-    case 2: return launch<float, 2>(a, pl, s);
-    case 3: return launch<float, 3>(a, pl, s);
-    case 4: return launch<float, 4>(a, pl, s);
-    case 5: return launch<float, 5>(a, pl, s);
-    case 6: return launch<float, 6>(a, pl, s);
-    case 7: return launch<float, 7>(a, pl, s);
-    case 8: return launch<float, 8>(a, pl, s);
+  if (pl.S > 1) {
+    const dim3 cols((unsigned)((size_t)a.r.B * a.p.Hkv * a.G * a.r.max_n));
+    if (dt == BF16)
+      hipLaunchKernelGGL(join_kernel<bf16>, cols, dim3(256), 0, s, a);
+    else
+      hipLaunchKernelGGL(join_kernel<float>, cols, dim3(256), 0, s, a);
   }
-  return hipErrorInvalidValue;
+  return hipGetLastError();
 }
 
 }  // namespace tadm
