@@ -36,7 +36,19 @@ __device__ __forceinline__ uint8_t code_of(float x, float inv) {
 }
 __device__ __forceinline__ float value_of(uint8_t c) { return __builtin_amdgcn_cvt_f32_fp8((int)c, 0); }
 
-// One block per (page of a row, K/V head, row).
+// 16 values from memory of any alignment
+template <class T>
+__device__ __forceinline__ void load16(const T* p, float (&x)[16]) {
+  T v[16];
+  __builtin_memcpy(v, p, sizeof v);
+#pragma unroll
+  for (int e = 0; e < 16; ++e) x[e] = f32_of(v[e]);
+}
+
+// One block per (page of a row, K/V head, row).  Up to 15 new positions a thread takes single
+// elements; from 16 on it takes units of 16 codes, all of a page in registers between the
+// search for the maximum and the rounding, so that the window is read once.  A unit
+// that holds other positions as well keeps theirs.
 template <class T>
 __global__ __launch_bounds__(256) void append_kernel(PageLayer p, PageRows r, const T* k, const T* vt, int cap) {
   __shared__ float red[2][4];
@@ -44,59 +56,125 @@ __global__ __launch_bounds__(256) void append_kernel(PageLayer p, PageRows r, co
   const int len = row_len(r, b);
   const int slot = len / PAGE + blockIdx.x, start = slot * PAGE;
   if (slot >= r.max_pages) return;
-  const int lo = max(len, start), hi = min(len + row_new(r, b), start + PAGE);
+  const int lo = max(len, start) - start, hi = min(len + row_new(r, b), start + PAGE) - start;  // new places of the page
   if (hi <= lo) return;
   const int page = r.table[(size_t)b * r.max_pages + slot];
   if ((unsigned)page >= (unsigned)p.n_pages) return;
-  const int m = hi - lo;
-  const T* ks = k + (((size_t)b * p.Hkv + h) * cap + (lo - len)) * dh;  // m rows of dh
-  const T* vs = vt + ((size_t)b * p.Hkv + h) * dh * cap + (lo - len);   // dh rows of m
-  float tk = 0.f, tv = 0.f;
-  for (int i = threadIdx.x; i < m * dh; i += 256) {
-    tk = fmaxf(tk, finite_abs(f32_of(ks[i])));
-    tv = fmaxf(tv, finite_abs(f32_of(vs[(size_t)(i / m) * cap + i % m])));
-  }
-  tk = wave_max(tk);
-  tv = wave_max(tv);
-  if (threadIdx.x % 64 == 0) {
-    red[0][threadIdx.x / 64] = tk;
-    red[1][threadIdx.x / 64] = tv;
-  }
-  __syncthreads();
+  // the window as the page sees it: place i of the page is token start - len + i
+  const T* ks = k + ((size_t)b * p.Hkv + h) * cap * dh + (ptrdiff_t)(start - len) * dh;
+  const T* vs = vt + ((size_t)b * p.Hkv + h) * dh * cap + (start - len);
   uint8_t* codes = p.data + (size_t)page * p.page_bytes + (size_t)h * 2 * PAGE * dh;
   float* scale = p.scale + (size_t)page * p.page_scales + 2 * h;
   const float old[2] = {scale[0], scale[1]};
-  __syncthreads();  // every thread has the old scales
+  const int m = hi - lo, units = 4 * dh;  // of a side; at most two a thread
+  const bool whole = m >= 16;
+  float x[2][2][16], top[2] = {0.f, 0.f};
+  if (whole) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int u = threadIdx.x + 256 * j;
+      if (u >= units) continue;
+      const int k0 = 16 * u / dh, k1 = (16 * u + 15) / dh;  // the unit's places
+      if (k0 >= lo && k1 < hi) {
+        load16(ks + 16 * u, x[0][j]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int at = (16 * u + e) / dh;
+          x[0][j][e] = at >= lo && at < hi ? f32_of(ks[16 * u + e]) : 0.f;
+        }
+      }
+      const int d = u / 4, v0 = 16 * (u % 4);
+      if (v0 >= lo && v0 + 16 <= hi) {
+        load16(vs + (size_t)d * cap + v0, x[1][j]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) x[1][j][e] = v0 + e >= lo && v0 + e < hi ? f32_of(vs[(size_t)d * cap + v0 + e]) : 0.f;
+      }
+#pragma unroll
+      for (int side = 0; side < 2; ++side)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) top[side] = fmaxf(top[side], finite_abs(x[side][j][e]));
+    }
+  } else {
+    for (int i = threadIdx.x; i < m * dh; i += 256) {
+      top[0] = fmaxf(top[0], finite_abs(f32_of(ks[lo * dh + i])));
+      top[1] = fmaxf(top[1], finite_abs(f32_of(vs[(size_t)(i / m) * cap + lo + i % m])));
+    }
+  }
+#pragma unroll
+  for (int side = 0; side < 2; ++side) {
+    top[side] = wave_max(top[side]);
+    if (threadIdx.x % 64 == 0) red[side][threadIdx.x / 64] = top[side];
+  }
+  __syncthreads();  // also: every thread has the old scales
 #pragma unroll
   for (int side = 0; side < 2; ++side) {
     float s = scale_of(fmaxf(fmaxf(red[side][0], red[side][1]), fmaxf(red[side][2], red[side][3])));
-    const int before = lo - start;  // earlier positions of the row on this page
     uint8_t* c = codes + side * PAGE * dh;
-    if (before > 0) {
-      if (s > old[side]) {  // the codes of the earlier positions at the larger scale
-        const float f = old[side] / s;
-        for (int i = threadIdx.x; i < before * dh; i += 256) {
-          uint8_t* at = side == 0 ? c + i : c + (i / before) * PAGE + i % before;
-          *at = (uint8_t)(__builtin_amdgcn_cvt_pk_fp8_f32(value_of(*at) * f, 0.f, 0, false) & 255);
+    const bool grown = lo > 0 && s > old[side];  // the codes of the earlier places change
+    if (lo > 0 && !grown) s = old[side];
+    const float inv = 1.f / s, f = old[side] * inv;
+    auto again = [&](uint8_t b) { return (uint8_t)(__builtin_amdgcn_cvt_pk_fp8_f32(value_of(b) * f, 0.f, 0, false) & 255); };
+    if (whole) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int u = threadIdx.x + 256 * j;
+        if (u >= units) continue;
+        const int first = side ? 16 * (u % 4) : 16 * u / dh, last = side ? first + 15 : (16 * u + 15) / dh;
+        const bool all = first >= lo && last < hi, none = last < lo || first >= hi;
+        if (none && !(grown && first < lo)) continue;
+        uint32_t w[4];
+        if (!all) *reinterpret_cast<uint4*>(w) = *reinterpret_cast<const uint4*>(c + 16 * u);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int at = side ? first + e : (16 * u + e) / dh, sh = 8 * (e % 4);
+          uint32_t b = (w[e / 4] >> sh) & 255u;
+          if (all || (at >= lo && at < hi))
+            b = code_of(x[side][j][e], inv);
+          else if (grown && at < lo)
+            b = again((uint8_t)b);
+          w[e / 4] = e % 4 ? (w[e / 4] & ~(255u << sh)) | (b << sh) : (w[e / 4] & ~255u) | b;
         }
-      } else {
-        s = old[side];
+        *reinterpret_cast<uint4*>(c + 16 * u) = *reinterpret_cast<const uint4*>(w);
       }
-    }
-    const float inv = 1.f / s;
-    for (int i = threadIdx.x; i < m * dh; i += 256) {
-      if (side == 0)
-        c[(size_t)before * dh + i] = code_of(f32_of(ks[i]), inv);
-      else
-        c[(i / m) * PAGE + before + i % m] = code_of(f32_of(vs[(size_t)(i / m) * cap + i % m]), inv);
+    } else {
+      if (grown)
+        for (int i = threadIdx.x; i < lo * dh; i += 256) {
+          uint8_t* at = side == 0 ? c + i : c + (i / lo) * PAGE + i % lo;
+          *at = again(*at);
+        }
+      for (int i = threadIdx.x; i < m * dh; i += 256) {
+        if (side == 0)
+          c[lo * dh + i] = code_of(f32_of(ks[lo * dh + i]), inv);
+        else
+          c[(i / m) * PAGE + lo + i % m] = code_of(f32_of(vs[(size_t)(i / m) * cap + lo + i % m]), inv);
+      }
     }
     if (threadIdx.x == 0) scale[side] = s;
   }
 }
 
-// One block per (page of a row, K/V head, row).
-template <class T>
+// W codes as values times the scale, 16 bytes of the model type: 8 for bf16, 4 for float
+__device__ __forceinline__ void values(const uint8_t* c, float s, bf16x8& v) {
+  const uint2 w = *reinterpret_cast<const uint2*>(c);
+  const auto p0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w.x, s, false),
+             p1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w.x, s, true),
+             p2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w.y, s, false),
+             p3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w.y, s, true);
+  v = bf16x8{p0[0], p0[1], p1[0], p1[1], p2[0], p2[1], p3[0], p3[1]};
+}
+__device__ __forceinline__ void values(const uint8_t* c, float s, f32x4& v) {
+  const int w = *reinterpret_cast<const int*>(c);
+  const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
+  v = f32x4{lo[0] * s, lo[1] * s, hi[0] * s, hi[1] * s};
+}
+
+// One block per (page of a row, K/V head, row); a thread takes pieces of 16 bytes of the result, so
+// that both sides move whole lines.
+template <class T, class V>
 __global__ __launch_bounds__(256) void read_kernel(PageLayer p, PageRows r, T* k, T* vt, int cap) {
+  constexpr int W = 16 / sizeof(T);
   const int b = blockIdx.z, h = blockIdx.y, dh = p.dh;
   const int start = blockIdx.x * PAGE, m = min(row_len(r, b) - start, PAGE);
   if (m <= 0) return;
@@ -107,10 +185,29 @@ __global__ __launch_bounds__(256) void read_kernel(PageLayer p, PageRows r, T* k
   const float sk = scale[0], sv = scale[1];
   T* kd = k + (((size_t)b * p.Hkv + h) * cap + start) * dh;
   T* vd = vt + ((size_t)b * p.Hkv + h) * dh * cap + start;
-  for (int i = threadIdx.x; i < m * dh; i += 256) {
-    kd[i] = from_f32<T>(there ? value_of(codes[i]) * sk : 0.f);
-    const int d = i / m, j = i % m;
-    vd[(size_t)d * cap + j] = from_f32<T>(there ? value_of(codes[PAGE * dh + d * PAGE + j]) * sv : 0.f);
+#pragma unroll 4
+  for (int u = threadIdx.x; u < PAGE * dh / W; u += 256) {
+    V x, y;
+    values(codes + W * u, sk, x);
+    values(codes + PAGE * dh + W * u, sv, y);
+    if (!there) x = y = V(0);
+    T* ko = kd + W * u;
+    if (W * u + W <= m * dh) {
+      *reinterpret_cast<V*>(ko) = x;
+    } else {
+#pragma unroll
+      for (int e = 0; e < W; ++e)
+        if (W * u + e < m * dh) ko[e] = x[e];
+    }
+    const int d = W * u / PAGE, j = W * u % PAGE;
+    T* vo = vd + (size_t)d * cap + j;
+    if (j + W <= m) {
+      *reinterpret_cast<V*>(vo) = y;
+    } else {
+#pragma unroll
+      for (int e = 0; e < W; ++e)
+        if (j + e < m) vo[e] = y[e];
+    }
   }
 }
 
@@ -178,10 +275,10 @@ hipError_t pages_read(DType dt, const PageLayer& p, const PageRows& r, void* k, 
   const dim3 grid((r.max_len + PAGE - 1) / PAGE, p.Hkv, r.B);
   if (grid.x == 0) return hipSuccess;
   if (dt == BF16)
-    hipLaunchKernelGGL(read_kernel<bf16>, grid, dim3(256), 0, s, p, r, static_cast<bf16*>(k), static_cast<bf16*>(vt),
+    hipLaunchKernelGGL((read_kernel<bf16, bf16x8>), grid, dim3(256), 0, s, p, r, static_cast<bf16*>(k), static_cast<bf16*>(vt),
                        cap);
   else
-    hipLaunchKernelGGL(read_kernel<float>, grid, dim3(256), 0, s, p, r, static_cast<float*>(k),
+    hipLaunchKernelGGL((read_kernel<float, f32x4>), grid, dim3(256), 0, s, p, r, static_cast<float*>(k),
                        static_cast<float*>(vt), cap);
   return hipGetLastError();
 }
