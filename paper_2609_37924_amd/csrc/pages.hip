@@ -26,24 +26,58 @@ __device__ __forceinline__ float scale_of(float top) {
   e = min(max(e, PAGE_E_MIN), PAGE_E_MAX);
   return __uint_as_float((uint32_t)(e + 127) << 23);
 }
-__device__ __forceinline__ float finite_abs(float x) {
-  const float a = fabsf(x);
-  return a < INFINITY ? a : 0.f;
+// The largest finite magnitude of values, by their bits: without the sign they order as the
+// values do, and adding one to the exponent makes those of infinities and NaN negative, which
+// a signed maximum that starts at 0 passes over.  bf16: two values a step.
+typedef short i16x2 __attribute__((ext_vector_type(2)));
+struct Top16 {
+  i16x2 m = {0x80, 0x80};
+  __device__ __forceinline__ void add(uint32_t two) {
+    const uint32_t t = two & 0x7fff7fffu;
+    m = __builtin_elementwise_max(m, __builtin_bit_cast(i16x2, t) + i16x2{0x80, 0x80});
+  }
+  __device__ __forceinline__ float value() const {
+    return __uint_as_float((uint32_t)(max((int)m[0], (int)m[1]) - 0x80) << 16);
+  }
+};
+struct Top32 {
+  int m = 0x800000;
+  __device__ __forceinline__ void add(uint32_t x) { m = max(m, (int)((x & 0x7fffffffu) + 0x800000u)); }
+  __device__ __forceinline__ float value() const { return __int_as_float(m - 0x800000); }
+};
+
+// 16 values as they lie in memory, of any alignment.
+template <class T>
+struct Raw16;
+template <>
+struct Raw16<bf16> {
+  typedef Top16 Top;
+  uint32_t w[8];
+  __device__ __forceinline__ float get(int e) const {
+    return __uint_as_float(e % 2 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
+  }
+  __device__ __forceinline__ void set(int e, bf16 x) {
+    const uint32_t b = __builtin_bit_cast(uint16_t, x);
+    w[e / 2] = e % 2 ? (w[e / 2] & 0xffffu) | b << 16 : (w[e / 2] & 0xffff0000u) | b;
+  }
+};
+template <>
+struct Raw16<float> {
+  typedef Top32 Top;
+  uint32_t w[16];
+  __device__ __forceinline__ float get(int e) const { return __uint_as_float(w[e]); }
+  __device__ __forceinline__ void set(int e, float x) { w[e] = __float_as_uint(x); }
+};
+
+// Codes of 4 values; one that is not finite gets a NaN code (nothing finite is above 448 here).
+__device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d, float inv) {
+  int v = __builtin_amdgcn_cvt_pk_fp8_f32(a * inv, b * inv, 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c * inv, d * inv, v, true);
 }
 __device__ __forceinline__ uint8_t code_of(float x, float inv) {
-  const int c = __builtin_amdgcn_cvt_pk_fp8_f32(x * inv, 0.f, 0, false) & 255;
-  return fabsf(x) < INFINITY ? c : 0x7f;
+  return (uint8_t)(__builtin_amdgcn_cvt_pk_fp8_f32(x * inv, 0.f, 0, false) & 255);
 }
 __device__ __forceinline__ float value_of(uint8_t c) { return __builtin_amdgcn_cvt_f32_fp8((int)c, 0); }
-
-// 16 values from memory of any alignment
-template <class T>
-__device__ __forceinline__ void load16(const T* p, float (&x)[16]) {
-  T v[16];
-  __builtin_memcpy(v, p, sizeof v);
-#pragma unroll
-  for (int e = 0; e < 16; ++e) x[e] = f32_of(v[e]);
-}
 
 // One block per (page of a row, K/V head, row).  Up to 15 new positions a thread takes single
 // elements; from 16 on it takes units of 16 codes, all of a page in registers between the
@@ -68,7 +102,8 @@ __global__ __launch_bounds__(256) void append_kernel(PageLayer p, PageRows r, co
   const float old[2] = {scale[0], scale[1]};
   const int m = hi - lo, units = 4 * dh;  // of a side; at most two a thread
   const bool whole = m >= 16;
-  float x[2][2][16], top[2] = {0.f, 0.f};
+  Raw16<T> x[2][2];  // [keys, values][unit]
+  typename Raw16<T>::Top tops[2];
   if (whole) {
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
@@ -76,36 +111,42 @@ __global__ __launch_bounds__(256) void append_kernel(PageLayer p, PageRows r, co
       if (u >= units) continue;
       const int k0 = 16 * u / dh, k1 = (16 * u + 15) / dh;  // the unit's places
       if (k0 >= lo && k1 < hi) {
-        load16(ks + 16 * u, x[0][j]);
+        __builtin_memcpy(x[0][j].w, ks + 16 * u, sizeof x[0][j].w);
       } else {
+        x[0][j] = Raw16<T>{};
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
           const int at = (16 * u + e) / dh;
-          x[0][j][e] = at >= lo && at < hi ? f32_of(ks[16 * u + e]) : 0.f;
+          if (at >= lo && at < hi) x[0][j].set(e, ks[16 * u + e]);
         }
       }
       const int d = u / 4, v0 = 16 * (u % 4);
       if (v0 >= lo && v0 + 16 <= hi) {
-        load16(vs + (size_t)d * cap + v0, x[1][j]);
+        __builtin_memcpy(x[1][j].w, vs + (size_t)d * cap + v0, sizeof x[1][j].w);
       } else {
+        x[1][j] = Raw16<T>{};
 #pragma unroll
-        for (int e = 0; e < 16; ++e) x[1][j][e] = v0 + e >= lo && v0 + e < hi ? f32_of(vs[(size_t)d * cap + v0 + e]) : 0.f;
+        for (int e = 0; e < 16; ++e)
+          if (v0 + e >= lo && v0 + e < hi) x[1][j].set(e, vs[(size_t)d * cap + v0 + e]);
       }
 #pragma unroll
       for (int side = 0; side < 2; ++side)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) top[side] = fmaxf(top[side], finite_abs(x[side][j][e]));
+        for (uint32_t w : x[side][j].w) tops[side].add(w);
     }
   } else {
     for (int i = threadIdx.x; i < m * dh; i += 256) {
-      top[0] = fmaxf(top[0], finite_abs(f32_of(ks[lo * dh + i])));
-      top[1] = fmaxf(top[1], finite_abs(f32_of(vs[(size_t)(i / m) * cap + lo + i % m])));
+      Raw16<T> one{};
+      one.set(0, ks[lo * dh + i]);
+      tops[0].add(one.w[0]);
+      one.set(0, vs[(size_t)(i / m) * cap + lo + i % m]);
+      tops[1].add(one.w[0]);
     }
   }
 #pragma unroll
   for (int side = 0; side < 2; ++side) {
-    top[side] = wave_max(top[side]);
-    if (threadIdx.x % 64 == 0) red[side][threadIdx.x / 64] = top[side];
+    const float top = wave_max(tops[side].value());
+    if (threadIdx.x % 64 == 0) red[side][threadIdx.x / 64] = top;
   }
   __syncthreads();  // also: every thread has the old scales
 #pragma unroll
@@ -124,17 +165,22 @@ __global__ __launch_bounds__(256) void append_kernel(PageLayer p, PageRows r, co
         const int first = side ? 16 * (u % 4) : 16 * u / dh, last = side ? first + 15 : (16 * u + 15) / dh;
         const bool all = first >= lo && last < hi, none = last < lo || first >= hi;
         if (none && !(grown && first < lo)) continue;
+        const Raw16<T>& v = x[side][j];
         uint32_t w[4];
-        if (!all) *reinterpret_cast<uint4*>(w) = *reinterpret_cast<const uint4*>(c + 16 * u);
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int at = side ? first + e : (16 * u + e) / dh, sh = 8 * (e % 4);
-          uint32_t b = (w[e / 4] >> sh) & 255u;
-          if (all || (at >= lo && at < hi))
-            b = code_of(x[side][j][e], inv);
-          else if (grown && at < lo)
-            b = again((uint8_t)b);
-          w[e / 4] = e % 4 ? (w[e / 4] & ~(255u << sh)) | (b << sh) : (w[e / 4] & ~255u) | b;
+        for (int e = 0; e < 4; ++e)
+          w[e] = codes4(v.get(4 * e), v.get(4 * e + 1), v.get(4 * e + 2), v.get(4 * e + 3), inv);
+        if (!all) {
+          uint32_t had[4];
+          *reinterpret_cast<uint4*>(had) = *reinterpret_cast<const uint4*>(c + 16 * u);
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const int at = side ? first + e : (16 * u + e) / dh, sh = 8 * (e % 4);
+            if (at >= lo && at < hi) continue;
+            uint32_t b = (had[e / 4] >> sh) & 255u;
+            if (grown && at < lo) b = again((uint8_t)b);
+            w[e / 4] = (w[e / 4] & ~(255u << sh)) | (b << sh);
+          }
         }
         *reinterpret_cast<uint4*>(c + 16 * u) = *reinterpret_cast<const uint4*>(w);
       }
