@@ -78,12 +78,14 @@ __device__ __forceinline__ Block block_of(const Args& a, int width) {
 // needs no rescaling.  Returns the factor for what was summed before.
 __device__ __forceinline__ float softmax_tile(f32x4 (&s)[4], int keys, int grp, float scale_log2, float& m, float& l) {
   float mt = -INFINITY;
-  if (keys < PAGE)
+  if (keys < PAGE) {
+    asm volatile("" : "+s"(keys));  // the comparisons stay in here
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
       for (int j = 0; j < 4; ++j)
         if (16 * grp + 4 * i + j >= keys) s[i][j] = -INFINITY;
+  }
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -275,6 +277,13 @@ __device__ __forceinline__ Query<DH> load_query(const bf16* q, int grp) {
   for (int c = 0; c < DH / 32; ++c) r.op[c] = *reinterpret_cast<const bf16x8*>(q + DH / 4 * grp + 8 * c);
   return r;
 }
+// Waits for a query's loads here.  Left to its first use, inside the loop over the tiles, the wait would
+// be for the tile's loads too, in every step.
+template <int DH>
+__device__ __forceinline__ void settle(Query<DH>& q) {
+#pragma unroll
+  for (int c = 0; c < DH / 32; ++c) asm volatile("" : "+v"(q.op[c]));
+}
 // Scores of QS strips of 16 columns and 16 keys, from the lane's DH / 4 codes of the row it stands for.
 // The codes become bf16, exactly, for the bf16 products: the 8-bit ones, twice as fast, drop
 // what lies 2^-12 below the largest product of a sum.
@@ -420,6 +429,8 @@ __global__ __launch_bounds__(256) void attend_narrow_kernel(Args a) {
   }
 #pragma unroll
   for (int u = 0; u < QS; ++u) qs[u] = load_query<DH>(q[u], grp);
+#pragma unroll
+  for (int u = 0; u < QS; ++u) settle<DH>(qs[u]);
   for (int st = 0; st < steps; ++st) {
     const int keys = at_lane(tb.keys, st & 63);
     const float sk = at_lane(tb.sk, st & 63), sv = at_lane(tb.sv, st & 63);
@@ -474,9 +485,9 @@ __global__ __launch_bounds__(256) void attend_narrow_kernel(Args a) {
 // instead of 47.5).  K row r of a stage has key 16 ((r / 4) % 4) + 4 (r / 16) + r % 4, the key
 // that score row r % 16 of block r / 16 stands for.  Chunk c (16 bytes) of row r sits in slot
 // c ^ (r & 7), so that 8 neighbouring lanes read different banks.
-template <int DH, int CW, int KW>
+template <int DH, int QS, int CW, int KW>
 __global__ __launch_bounds__(64 * CW * KW, 2) void attend_wide_kernel(Args a) {
-  constexpr int QS = 2, NB = DH / 16, KC = DH / 16, NV = 2 + 4 * NB, GT = 64 * CW;
+  constexpr int NB = DH / 16, KC = DH / 16, NV = 2 + 4 * NB, GT = 64 * CW;
   constexpr int SIDE = PAGE * DH, KBYTES = 2 * SIDE, STAGE = 2 * KBYTES;
   constexpr int PER = SIDE / 16 / GT;  // chunks of a side that a lane moves per tile
   static_assert(PER * 16 * GT == SIDE, "a tile splits over the lanes of a group");
@@ -554,6 +565,8 @@ __global__ __launch_bounds__(64 * CW * KW, 2) void attend_wide_kernel(Args a) {
   for (int e = 0; e < 2; ++e) {
     vofs[e] = KBYTES + fr * 128 + ((2 * grp + e) ^ (fr & 7)) * 16;
   }
+#pragma unroll
+  for (int u = 0; u < QS; ++u) settle<DH>(qs[u]);
   for (int st = 0; st < steps; ++st) {
     keys = keys_next;
     __syncthreads();  // the step's stage is written, and the other one read
@@ -718,7 +731,7 @@ void start(K kernel, const Args& a, const Plan& p, int threads, hipStream_t s) {
 template <int DH>
 void start_bf16(const Args& a, const Plan& p, hipStream_t s) {
   if (p.cw)
-    p.kw == 2 ? start(attend_wide_kernel<DH, 4, 2>, a, p, 512, s) : start(attend_wide_kernel<DH, 4, 1>, a, p, 256, s);
+    p.kw == 2 ? start(attend_wide_kernel<DH, 2, 4, 2>, a, p, 512, s) : start(attend_wide_kernel<DH, 2, 4, 1>, a, p, 256, s);
   else
     p.width == 32 ? start(attend_narrow_kernel<DH, 2>, a, p, 256, s) : start(attend_narrow_kernel<DH, 1>, a, p, 256, s);
 }
