@@ -7,9 +7,8 @@
 // lie one after the other in memory), so that a page is read once for all of them.  Scores
 // are computed transposed, S^T = K Q^T, a lane owning one column; the running maximum and sum
 // of the softmax live in the lane, and the probabilities feed O^T = V^T P^T from registers.
-// The order of the keys within a page is free (a sum over them): score row 4 g + j of the
-// 16-key block i stands for key 16 g + 4 i + j, so that a lane's 16 probabilities of a page
-// are those of 16 consecutive keys, one 16-byte load of a V^T row.
+// The order of the keys within a page is free (a sum over them), and so is that of the head
+// width within a score: each kernel takes the orders that its loads of K and V^T like best.
 //
 // Three kernels: float32 models; bf16 with few columns, where each wave takes tiles of 64 keys
 // of its own straight from memory (the pages' bytes bound it); bf16 with many, where tiles
@@ -72,10 +71,18 @@ __device__ __forceinline__ Block block_of(const Args& a, int width) {
   return x;
 }
 
-// One tile of a column's softmax.  s[i][j]: the score of key 16 grp + 4 i + j, unscaled; on
+// The key of a tile that row 4 grp + j of its i-th block of 16 scores stands for.  RUN: 16 keys in a row
+// for a lane, one 16-byte load of the codes of a V^T row; else two runs of 8, 32 apart.
+template <bool RUN>
+__device__ __forceinline__ int key_of(int i, int grp, int j) {
+  return RUN ? 16 * grp + 4 * i + j : 32 * (i >> 1) + 8 * grp + 4 * (i & 1) + j;
+}
+
+// One tile of a column's softmax.  s[i][j]: the score of key_of(i, grp, j), unscaled; on
 // return its probability relative to a reference m (base 2) that moves only when the tile's
 // maximum exceeds it by more than 2^8: until then the probabilities stay below 256 and O
 // needs no rescaling.  Returns the factor for what was summed before.
+template <bool RUN>
 __device__ __forceinline__ float softmax_tile(f32x4 (&s)[4], int keys, int grp, float scale_log2, float& m, float& l) {
   float mt = -INFINITY;
   if (keys < PAGE) {
@@ -84,7 +91,7 @@ __device__ __forceinline__ float softmax_tile(f32x4 (&s)[4], int keys, int grp, 
     for (int i = 0; i < 4; ++i)
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        if (16 * grp + 4 * i + j >= keys) s[i][j] = -INFINITY;
+        if (key_of<RUN>(i, grp, j) >= keys) s[i][j] = -INFINITY;
   }
 #pragma unroll
   for (int i = 0; i < 4; ++i)
@@ -221,7 +228,7 @@ __global__ __launch_bounds__(256) void attend_f32_kernel(Args a) {
     f32x4 s[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int key = 16 * (fr >> 2) + 4 * i + (fr & 3);
+      const int key = key_of<true>(i, fr >> 2, fr & 3);
       s[i] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int c = 0; c < NB; ++c) {
@@ -233,7 +240,7 @@ __global__ __launch_bounds__(256) void attend_f32_kernel(Args a) {
         for (int e = 0; e < 4; ++e) s[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[e], qx[c][e], s[i], 0, 0, 0);
       }
     }
-    const float alpha = softmax_tile(s, keys, grp, a.scale_log2, m_run, l_run);
+    const float alpha = softmax_tile<true>(s, keys, grp, a.scale_log2, m_run, l_run);
     // V^T row 16 d + fr, keys 16 grp + [0, 16); what lies behind the last key is taken as 0, so
     // that p = 0 meets a finite value
 #pragma unroll
@@ -265,16 +272,17 @@ __device__ __forceinline__ bf16x8 bf16_codes(uint32_t a, uint32_t b, float s) {
              p3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, s, true);
   return bf16x8{p0[0], p0[1], p1[0], p1[1], p2[0], p2[1], p3[0], p3[1]};
 }
-// A column's query: a lane has the elements [W grp, + W), W = DH / 4, of its column.
+// A column's query.  RUN: a lane has DH / 4 elements in a row; else runs of 8, 32 apart.
 template <int DH>
 struct Query {
   bf16x8 op[DH / 32];
 };
-template <int DH>
+template <int DH, bool RUN>
 __device__ __forceinline__ Query<DH> load_query(const bf16* q, int grp) {
   Query<DH> r;
 #pragma unroll
-  for (int c = 0; c < DH / 32; ++c) r.op[c] = *reinterpret_cast<const bf16x8*>(q + DH / 4 * grp + 8 * c);
+  for (int c = 0; c < DH / 32; ++c)
+    r.op[c] = *reinterpret_cast<const bf16x8*>(q + (RUN ? DH / 4 * grp + 8 * c : 32 * c + 8 * grp));
   return r;
 }
 // Waits for a query's loads here.  Left to its first use, inside the loop over the tiles, the wait would
@@ -323,8 +331,8 @@ __device__ __forceinline__ float at_lane(float v, int lane) {
   return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane));
 }
 
-// Probabilities of a tile as the operand of O^T = V^T P^T: k index 8 grp + j of product c is key
-// 16 grp + 8 c + j.
+// Probabilities of a tile as the operand of O^T = V^T P^T: k index 8 grp + j of product c is the key of
+// score row 4 grp + j % 4 of block 2 c + j / 4.
 __device__ __forceinline__ void p_operand(const f32x4 (&s)[4], bf16x8 (&p)[2]) {
 #pragma unroll
   for (int c = 0; c < 2; ++c)
@@ -352,7 +360,7 @@ __device__ __forceinline__ void window_tile(const Args& a, const Block& x, int w
     for (int u = 0; u < QS; ++u) qf[u] = *reinterpret_cast<const bf16x8*>(q[u] + 32 * c + 8 * grp);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int key = 16 * (fr >> 2) + 4 * i + (fr & 3);
+      const int key = key_of<true>(i, fr >> 2, fr & 3);
       const bf16x8 kf = *reinterpret_cast<const bf16x8*>(kw + (size_t)key * DH + 32 * c + 8 * grp);
 #pragma unroll
       for (int u = 0; u < QS; ++u) s[u][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[u], s[u][i], 0, 0, 0);
@@ -361,7 +369,7 @@ __device__ __forceinline__ void window_tile(const Args& a, const Block& x, int w
   bf16x8 p[QS][2];
 #pragma unroll
   for (int u = 0; u < QS; ++u) {
-    const float alpha = softmax_tile(s[u], keys, grp, a.scale_log2, m_run[u], l_run[u]);
+    const float alpha = softmax_tile<true>(s[u], keys, grp, a.scale_log2, m_run[u], l_run[u]);
     if (__builtin_amdgcn_ballot_w64(alpha != 1.f))
 #pragma unroll
       for (int d = 0; d < NB; ++d) o[u][d] *= alpha;
@@ -407,7 +415,7 @@ __global__ __launch_bounds__(256) void attend_narrow_kernel(Args a) {
   }
   TileBatch tb = tile_batch(a, x, first + NW * lane, tp);
   const uint8_t* base = a.p.data + (size_t)x.h * 2 * PAGE * DH;
-  const int koff = (16 * (fr >> 2) + (fr & 3)) * DH + DH / 4 * grp;
+  const int koff = key_of<true>(0, fr >> 2, fr & 3) * DH + DH / 4 * grp;
   const int voff = PAGE * DH + fr * PAGE + 16 * grp;
   uint4 kc[4][DH / 64], vc[NB];
   auto load_k = [&](int page) {
@@ -428,7 +436,7 @@ __global__ __launch_bounds__(256) void attend_narrow_kernel(Args a) {
     load_v(page);
   }
 #pragma unroll
-  for (int u = 0; u < QS; ++u) qs[u] = load_query<DH>(q[u], grp);
+  for (int u = 0; u < QS; ++u) qs[u] = load_query<DH, true>(q[u], grp);
 #pragma unroll
   for (int u = 0; u < QS; ++u) settle<DH>(qs[u]);
   for (int st = 0; st < steps; ++st) {
@@ -446,7 +454,7 @@ __global__ __launch_bounds__(256) void attend_narrow_kernel(Args a) {
     bf16x8 p[QS][2];
 #pragma unroll
     for (int u = 0; u < QS; ++u) {
-      const float alpha = softmax_tile(s[u], keys, grp, a.scale_log2, m_run[u], l_run[u]);
+      const float alpha = softmax_tile<true>(s[u], keys, grp, a.scale_log2, m_run[u], l_run[u]);
       if (__builtin_amdgcn_ballot_w64(alpha != 1.f))
 #pragma unroll
         for (int d = 0; d < NB; ++d) o[u][d] *= alpha;
@@ -476,175 +484,204 @@ __global__ __launch_bounds__(256) void attend_narrow_kernel(Args a) {
     join_waves<bf16, NB, NW>(a, x, x.ct * 16 * QS + 16 * u + fr, m_run[u], l_run[u], o[u], xs);
 }
 
-// Many columns: CW waves with 32 columns each share the tiles of pages in LDS; KW such groups take
-// every KW-th tile and are joined at the end.  Two stages: while one tile is computed, the codes
-// of the next are on their way to registers, from which they go to the other stage as bf16,
-// scaled, the values 0 behind the last key, so that p = 0 meets a finite value: a wave converts
-// its share of a tile once for all of them (with the keys as codes in LDS, converted by
-// every wave, 4 x 256 columns over 16K take 408 us instead of 379, 16 x 64 over 1K 59
-// instead of 47.5).  K row r of a stage has key 16 ((r / 4) % 4) + 4 (r / 16) + r % 4, the key
-// that score row r % 16 of block r / 16 stands for.  Chunk c (16 bytes) of row r sits in slot
-// c ^ (r & 7), so that 8 neighbouring lanes read different banks.
-template <int DH, int QS, int CW, int KW>
-__global__ __launch_bounds__(64 * CW * KW, 2) void attend_wide_kernel(Args a) {
-  constexpr int NB = DH / 16, KC = DH / 16, NV = 2 + 4 * NB, GT = 64 * CW;
-  constexpr int SIDE = PAGE * DH, KBYTES = 2 * SIDE, STAGE = 2 * KBYTES;
-  constexpr int PER = SIDE / 16 / GT;  // chunks of a side that a lane moves per tile
-  static_assert(PER * 16 * GT == SIDE, "a tile splits over the lanes of a group");
-  constexpr int RING = 2 * KW * STAGE, MERGE = KW > 1 ? CW * NV * 64 * 4 : 0;
-  __shared__ __attribute__((aligned(16))) char smem[RING > MERGE ? RING : MERGE];
+// Slot of chunk c (16 bytes) of a row of 128 or 256 bytes in LDS: c ^ swizzle(row).  With it, and lane
+// group g at chunk 4 c + g, reads of 16 rows meet the banks evenly (4 cycles a wave, 8 with
+// the groups' chunks side by side), and so do writes of a row's chunks by neighbouring lanes.
+template <int ROW>
+__device__ __forceinline__ int swizzle(int row) {
+  static_assert(ROW == 128 || ROW == 256, "bytes of a row");
+  return row & (ROW / 16 - 1);
+}
+
+// Many columns: two groups of CW waves work on the same 16 QS CW columns, each on every second tile of
+// 64 keys, which its waves share through LDS.  The groups take turns: while one is at its
+// matrix products (O += V^T P of the tile before, S = K Q^T of this one), the other is at its
+// exponentials, so that each SIMD has a wave for its matrix core and one for its vector unit.
+// A barrier of the whole block ends every such half step.  The next tile's K goes to LDS
+// beside the matrix products and its V, used a step later, beside the exponentials.
+//
+// The codes of a tile are converted to bf16, scaled, on their way to LDS, once for all waves
+// (with codes in LDS, converted by every wave, the step took 8 % more), the values 0 behind the
+// last key, so that p = 0 meets a finite value.  K row r has the key that score row r % 16 of
+// block r / 16 stands for.
+template <int DH, int QS, int CW>
+__global__ __launch_bounds__(128 * CW, 2) void attend_wide_kernel(Args a) {
+  constexpr int NB = DH / 16, KC = DH / 8, NV = 2 + 4 * NB, GT = 64 * CW;
+  constexpr int SIDE = PAGE * DH, BUF = 2 * SIDE, GROUP = 4 * BUF;  // codes of a side, and its bf16; K, K, V, V
+  constexpr int PER = SIDE / 8 / GT;                               // chunks (8 codes) of a side that a lane moves per tile
+  constexpr int KROWS = GT / KC, VROWS = GT / 8;                   // rows of K and V^T that a group moves at once
+  static_assert(PER * 8 * GT == SIDE && CW == 4, "a tile splits over the lanes of a group in whole blocks of 16 keys");
+  static_assert(CW * NV * 64 * 4 <= 2 * GROUP, "the groups are joined in the space of the tiles");
+  __shared__ __attribute__((aligned(16))) char smem[2 * GROUP];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), grp = lane >> 4,
             fr = lane & 15, cw = wave % CW, kw = wave / CW, gl = cw * 64 + lane;
   const Block x = block_of(a, 16 * QS * CW);
   if (x.n == 0) return;
-  const int ncol = a.G * a.r.max_n, tp = min(x.t1, x.np), col0 = (x.ct * CW + cw) * 16 * QS;
-  const int steps = x.t0 < tp ? (tp - x.t0 + KW - 1) / KW : 0;  // of every wave; a group may have no tile in the last
-  const bf16* q[QS];
+  const int ncol = a.G * a.r.max_n, col0 = (x.ct * CW + cw) * 16 * QS;
+  const int tp = min(x.t1, x.np);
+  const int steps = x.t0 < tp ? (tp - x.t0 + 1) / 2 : 0;  // of both groups; the second may have no tile in the last
   Query<DH> qs[QS];
-  f32x4 o[QS][NB];
+  f32x4 o[QS][NB], s[QS][4];
+  bf16x8 p[QS][2];
   float m_run[QS], l_run[QS];
 #pragma unroll
   for (int u = 0; u < QS; ++u) {
-    q[u] = static_cast<const bf16*>(a.q) + (x.head * ncol + min(col0 + 16 * u + fr, ncol - 1)) * DH;
     m_run[u] = -INFINITY;
     l_run[u] = 0.f;
 #pragma unroll
     for (int d = 0; d < NB; ++d) o[u][d] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  // the lane's chunks of a tile: where they come from and where they go
-  int k_src[PER], k_dst[PER][2], v_dst[PER][2];
-#pragma unroll
-  for (int j = 0; j < PER; ++j) {
-    const int id = gl + GT * j, r = id / KC, c = id % KC;
-    k_src[j] = (16 * ((r >> 2) & 3) + 4 * (r >> 4) + (r & 3)) * DH + c * 16;
-#pragma unroll
-    for (int e = 0; e < 2; ++e) k_dst[j][e] = r * 2 * DH + ((2 * c + e) ^ (r & 7)) * 16;
-#pragma unroll
-    for (int e = 0; e < 2; ++e) v_dst[j][e] = KBYTES + (id / 4) * 128 + ((2 * (id % 4) + e) ^ (id / 4 & 7)) * 16;
-  }
+  // the lane's chunks of a tile: the j-th is KROWS j rows of K, VROWS j rows of V^T after the first
   const uint8_t* base = a.p.data + (size_t)x.h * 2 * PAGE * DH;
-  TileBatch tb = tile_batch(a, x, x.t0 + kw + KW * lane, tp);
-  uint4 kc[PER], vc[PER];
-  int keys = 0, keys_next = 0;
+  char* const sb = smem + kw * GROUP;
+  const int kr = gl / KC, vr = gl / 8;
+  const int k_src = key_of<false>(kr >> 4, kr >> 2 & 3, kr & 3) * DH + gl % KC * 8;
+  const int k_dst = kr * 2 * DH + (gl % KC ^ swizzle<2 * DH>(kr)) * 16;
+  const int v_dst = 2 * BUF + vr * 128 + (gl % 8 ^ swizzle<128>(vr)) * 16;
+  auto k_next = [&](int j) { return key_of<false>(KROWS * j >> 4, 0, 0) * DH; };
+  TileBatch tb = tile_batch(a, x, x.t0 + kw + 2 * lane, tp);
+  uint2 kc[PER], vc[PER];
+  int page = 0, keys = 0, keys_next = 0;
   float sk_next = 1.f, sv_next = 1.f;
-  auto load = [&](int st) {
-    if (st && (st & 63) == 0) tb = tile_batch(a, x, x.t0 + kw + KW * (st + lane), tp);
-    keys_next = at_lane(tb.keys, st & 63);
+  auto load_k = [&](int st) {
+    if (st && (st & 63) == 0) tb = tile_batch(a, x, x.t0 + kw + 2 * (st + lane), tp);
+    page = at_lane(tb.page, st & 63);
     sk_next = at_lane(tb.sk, st & 63);
+    const uint8_t* c = base + (size_t)page * a.p.page_bytes;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) kc[j] = *reinterpret_cast<const uint2*>(c + k_src + k_next(j));
+  };
+  auto load_v = [&](int st) {
+    keys_next = at_lane(tb.keys, st & 63);
     sv_next = at_lane(tb.sv, st & 63);
-    const uint8_t* c = base + (size_t)at_lane(tb.page, st & 63) * a.p.page_bytes;
+    const uint8_t* c = base + (size_t)page * a.p.page_bytes;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) vc[j] = *reinterpret_cast<const uint2*>(c + SIDE + (gl + GT * j) * 8);
+  };
+  auto place_k = [&](int st) {
+    char* to = sb + (st & 1) * BUF + k_dst;
+#pragma unroll
+    for (int j = 0; j < PER; ++j)
+      *reinterpret_cast<bf16x8*>(to + KROWS * j * 2 * DH) = bf16_codes(kc[j].x, kc[j].y, sk_next);
+  };
+  auto place_v = [&](int st) {
+    char* to = sb + (st & 1) * BUF + v_dst;
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
-      kc[j] = *reinterpret_cast<const uint4*>(c + k_src[j]);
-      vc[j] = *reinterpret_cast<const uint4*>(c + SIDE + (gl + GT * j) * 16);
+      uint2 w = vc[j];
+      if (keys_next < PAGE) w = uint2{keep_bytes(w.x, keys_next - gl % 8 * 8), keep_bytes(w.y, keys_next - gl % 8 * 8 - 4)};
+      *reinterpret_cast<bf16x8*>(to + VROWS * j * 128) = bf16_codes(w.x, w.y, sv_next);
     }
   };
-  auto place = [&](int st) {
-    char* sb = smem + ((st & 1) * KW + kw) * STAGE;
-#pragma unroll
-    for (int j = 0; j < PER; ++j) {
-      *reinterpret_cast<bf16x8*>(sb + k_dst[j][0]) = bf16_codes(kc[j].x, kc[j].y, sk_next);
-      *reinterpret_cast<bf16x8*>(sb + k_dst[j][1]) = bf16_codes(kc[j].z, kc[j].w, sk_next);
-      uint32_t w[4] = {vc[j].x, vc[j].y, vc[j].z, vc[j].w};
-      if (keys_next < PAGE)  // what lies behind the last key is taken as 0, so that p = 0 meets a finite value
-#pragma unroll
-        for (int c = 0; c < 4; ++c) w[c] = keep_bytes(w[c], keys_next - 16 * (gl & 3) - 4 * c);
-      *reinterpret_cast<bf16x8*>(sb + v_dst[j][0]) = bf16_codes(w[0], w[1], sv_next);
-      *reinterpret_cast<bf16x8*>(sb + v_dst[j][1]) = bf16_codes(w[2], w[3], sv_next);
-    }
-  };
-  if (steps) load(0);
-#pragma unroll
-  for (int u = 0; u < QS; ++u) qs[u] = load_query<DH>(q[u], grp);
-  if (steps) place(0);
-  // the lane's places in a stage: K row fr (the chunks of its codes), V^T row fr (keys 16 grp + 8 c + [0, 8))
+  // the lane's places in a buffer: K row fr, chunks 4 e + grp; V^T row fr, chunks (8 keys) 4 c + grp
   int kofs[DH / 32], vofs[2];
 #pragma unroll
-  for (int e = 0; e < DH / 32; ++e) kofs[e] = fr * 2 * DH + ((DH / 32 * grp + e) ^ (fr & 7)) * 16;
+  for (int e = 0; e < DH / 32; ++e) kofs[e] = fr * 2 * DH + ((4 * e + grp) ^ swizzle<2 * DH>(fr)) * 16;
 #pragma unroll
-  for (int e = 0; e < 2; ++e) {
-    vofs[e] = KBYTES + fr * 128 + ((2 * grp + e) ^ (fr & 7)) * 16;
+  for (int e = 0; e < 2; ++e) vofs[e] = 2 * BUF + fr * 128 + ((4 * e + grp) ^ swizzle<128>(fr)) * 16;
+  auto add_pv = [&](int st) {  // O += V^T P of step st
+    const char* sv = sb + (st & 1) * BUF;
+#pragma unroll
+    for (int d = 0; d < NB; ++d)
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const bf16x8 vf = *reinterpret_cast<const bf16x8*>(sv + d * 16 * 128 + vofs[c]);
+#pragma unroll
+        for (int u = 0; u < QS; ++u) o[u][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, p[u][c], o[u][d], 0, 0, 0);
+      }
+  };
+  const bf16* q[QS];
+#pragma unroll
+  for (int u = 0; u < QS; ++u)
+    q[u] = static_cast<const bf16*>(a.q) + (x.head * ncol + min(col0 + 16 * u + fr, ncol - 1)) * DH;
+  if (steps) {
+    load_k(0);
+    load_v(0);
+#pragma unroll
+    for (int u = 0; u < QS; ++u) qs[u] = load_query<DH, false>(q[u], grp);
+    place_k(0);
+    place_v(0);
+    keys = keys_next;
+    if (steps > 1) {
+      load_k(1);
+      load_v(1);
+    }
   }
 #pragma unroll
   for (int u = 0; u < QS; ++u) settle<DH>(qs[u]);
+  if (kw) __syncthreads();  // the second group is half a step behind
   for (int st = 0; st < steps; ++st) {
-    keys = keys_next;
-    __syncthreads();  // the step's stage is written, and the other one read
-    if (st + 1 < steps) load(st + 1);
-    if (keys > 0) {
-      const char* sb = smem + ((st & 1) * KW + kw) * STAGE;
-      f32x4 s[QS][4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-#pragma unroll
-        for (int u = 0; u < QS; ++u) s[u][i] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int e = 0; e < DH / 32; ++e) {
-          const bf16x8 k = *reinterpret_cast<const bf16x8*>(sb + i * 32 * DH + kofs[e]);
-#pragma unroll
-          for (int u = 0; u < QS; ++u)
-            s[u][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, qs[u].op[e], s[u][i], 0, 0, 0);
-        }
-      }
-      bf16x8 p[QS][2];
-#pragma unroll
-      for (int u = 0; u < QS; ++u) {
-        const float alpha = softmax_tile(s[u], keys, grp, a.scale_log2, m_run[u], l_run[u]);
-        if (__builtin_amdgcn_ballot_w64(alpha != 1.f))
-#pragma unroll
-          for (int d = 0; d < NB; ++d) o[u][d] *= alpha;
-        p_operand(s[u], p[u]);
-      }
-#pragma unroll
-      for (int d = 0; d < NB; ++d)
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          const bf16x8 vf = *reinterpret_cast<const bf16x8*>(sb + d * 16 * 128 + vofs[c]);
-#pragma unroll
-          for (int u = 0; u < QS; ++u) o[u][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, p[u][c], o[u][d], 0, 0, 0);
-        }
+    __syncthreads();  // the group's K of this step and V of the one before are in LDS
+    if (st + 1 < steps) {
+      place_k(st + 1);
+      if (st + 2 < steps) load_k(st + 2);
     }
-    if (st + 1 < steps) place(st + 1);
+    if (st) add_pv(st - 1);
+    const char* sk = sb + (st & 1) * BUF;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+#pragma unroll
+      for (int u = 0; u < QS; ++u) s[u][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int e = 0; e < DH / 32; ++e) {
+        const bf16x8 k = *reinterpret_cast<const bf16x8*>(sk + i * 32 * DH + kofs[e]);
+#pragma unroll
+        for (int u = 0; u < QS; ++u) s[u][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, qs[u].op[e], s[u][i], 0, 0, 0);
+      }
+    }
+    __syncthreads();  // the group is done with V of the step before
+    const int keys_now = keys;
+    if (st + 1 < steps) {
+      place_v(st + 1);
+      keys = keys_next;
+      if (st + 2 < steps) load_v(st + 2);
+    }
+#pragma unroll
+    for (int u = 0; u < QS; ++u) {
+      const float alpha = softmax_tile<false>(s[u], keys_now, grp, a.scale_log2, m_run[u], l_run[u]);
+      if (__builtin_amdgcn_ballot_w64(alpha != 1.f))
+#pragma unroll
+        for (int d = 0; d < NB; ++d) o[u][d] *= alpha;
+      p_operand(s[u], p[u]);
+    }
   }
+  __syncthreads();
+  if (steps) add_pv(steps - 1);
+  if (!kw) __syncthreads();
   for (int t = max(x.t0, x.np); t < x.t1; ++t)
-    if ((t - x.t0) % KW == kw) window_tile<DH, QS>(a, x, t - x.np, q, o, m_run, l_run);
+    if (((t - x.t0) & 1) == kw) window_tile<DH, QS>(a, x, t - x.np, q, o, m_run, l_run);
+  // the second group joins the first, a strip at a time
+  float* w = reinterpret_cast<float*>(smem) + cw * NV * 64 + lane;
 #pragma unroll
   for (int u = 0; u < QS; ++u) {
     float l = l_run[u] + xor16(l_run[u]);
     l_run[u] = l + xor32(l);
-    if constexpr (KW > 1) {  // the second group joins the first, a strip at a time
-      static_assert(KW <= 2, "two key groups");
-      float* w = reinterpret_cast<float*>(smem) + cw * NV * 64 + lane;
-      __syncthreads();  // every wave is done with the ring, or with the previous strip
-      if (kw == 1) {
-        w[0] = m_run[u];
-        w[64] = l_run[u];
+    __syncthreads();  // every wave is done with the tiles, or with the previous strip
+    if (kw == 1) {
+      w[0] = m_run[u];
+      w[64] = l_run[u];
 #pragma unroll
-        for (int d = 0; d < NB; ++d)
+      for (int d = 0; d < NB; ++d)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) w[(2 + 4 * d + j) * 64] = o[u][d][j];
-      }
-      __syncthreads();
-      if (kw == 0) {
-        const float m = fmaxf(m_run[u], w[0]), ref = m == -INFINITY ? 0.f : m;
-        const float f0 = __builtin_amdgcn_exp2f(m_run[u] - ref), f1 = __builtin_amdgcn_exp2f(w[0] - ref);
-        l_run[u] = l_run[u] * f0 + w[64] * f1;
-        m_run[u] = m;
-#pragma unroll
-        for (int d = 0; d < NB; ++d)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) o[u][d][j] = o[u][d][j] * f0 + w[(2 + 4 * d + j) * 64] * f1;
-      }
+        for (int j = 0; j < 4; ++j) w[(2 + 4 * d + j) * 64] = o[u][d][j];
     }
-    const int col = col0 + 16 * u + fr;
-    if (kw == 0 && col < ncol && col % a.r.max_n < x.n) {
-      const float inv = inverse(a, l_run[u]);
+    __syncthreads();
+    if (kw == 0) {
+      const float m = fmaxf(m_run[u], w[0]), ref = m == -INFINITY ? 0.f : m;
+      const float f0 = __builtin_amdgcn_exp2f(m_run[u] - ref), f1 = __builtin_amdgcn_exp2f(w[0] - ref);
+      const float l = l_run[u] * f0 + w[64] * f1;
+      const int col = col0 + 16 * u + fr;
+      if (col < ncol && col % a.r.max_n < x.n) {
+        const float inv = inverse(a, l);
 #pragma unroll
-      for (int d = 0; d < NB; ++d) {
-        const float r[4] = {o[u][d][0], o[u][d][1], o[u][d][2], o[u][d][3]};
-        put4<bf16>(a, x, col, 16 * d + 4 * grp, inv, r);
+        for (int d = 0; d < NB; ++d) {
+          float r[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) r[j] = o[u][d][j] * f0 + w[(2 + 4 * d + j) * 64] * f1;
+          put4<bf16>(a, x, col, 16 * d + 4 * grp, inv, r);
+        }
+        if (grp == 0) put_ml(a, x, col, m, l);
       }
-      if (grp == 0) put_ml(a, x, col, m_run[u], l_run[u]);
     }
   }
 }
@@ -694,29 +731,24 @@ __global__ __launch_bounds__(256) void join_kernel(Args a) {
   if (threadIdx.x == 0 && a.lse) a.lse[col_id] = sum == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * LN2;
 }
 
-// Which kernel a call takes: columns of a block, waves along the columns and the keys, splits.
-// Which kernel a call takes: columns of a block, waves along the columns and the keys, splits.
-// Which kernel a call takes: columns of a block, waves along the columns and the keys, splits.
-// Which kernel a call takes: columns of a block, waves along the columns and the keys, splits.
-// Which kernel a call takes: columns of a block, waves along the columns and the keys, splits.
-// Which kernel a call takes: columns of a block, waves along the columns and the keys, splits.
+// Which kernel a call takes: columns of a block, tiles that its waves work on at once, splits.
 struct Plan {
-  int width, cw, kw, S;
+  int width, waves, S;
 };
 
 Plan plan(DType dt, int B, int H, int Hkv, int L, int max_len) {
   const int ncol = H / Hkv * L;
   const int tiles = (max_len + PAGE - 1) / PAGE + (L + PAGE - 1) / PAGE;
   auto blocks = [&](int width) { return (long)B * Hkv * ((ncol + width - 1) / width); };
-  Plan p{16, 0, 4, 1};
-  if (dt == BF16 && ncol > 32) {
-    p = Plan{128, 4, 1, 1};
-    if (blocks(128) < 512) p.kw = 2;
+  Plan p{16, 4, 1};
+  const bool wide = dt == BF16 && ncol > 32;
+  if (wide) {
+    p = Plan{blocks(128) < 256 ? 64 : 128, 2, 1};
   } else if (dt == BF16 && ncol > 16) {
     p.width = 32;
   }
-  const long n = blocks(p.width), most = (tiles + 4 * p.kw - 1) / (4 * p.kw);  // four tiles per wave at least
-  long S = (p.cw ? 512 / p.kw : 768) / n;
+  const long n = blocks(p.width), most = (tiles + 4 * p.waves - 1) / (4 * p.waves);  // four tiles per wave at least
+  long S = (wide ? 256 : 768) / n;
   S = S < most ? S : most;
   p.S = S < 1 ? 1 : (int)S;
   return p;
@@ -730,10 +762,12 @@ void start(K kernel, const Args& a, const Plan& p, int threads, hipStream_t s) {
 
 template <int DH>
 void start_bf16(const Args& a, const Plan& p, hipStream_t s) {
-  if (p.cw)
-    p.kw == 2 ? start(attend_wide_kernel<DH, 2, 4, 2>, a, p, 512, s) : start(attend_wide_kernel<DH, 2, 4, 1>, a, p, 256, s);
-  else
-    p.width == 32 ? start(attend_narrow_kernel<DH, 2>, a, p, 256, s) : start(attend_narrow_kernel<DH, 1>, a, p, 256, s);
+  switch (p.width) {
+    case 128: return start(attend_wide_kernel<DH, 2, 4>, a, p, 512, s);
+    case 64: return start(attend_wide_kernel<DH, 1, 4>, a, p, 512, s);
+    case 32: return start(attend_narrow_kernel<DH, 2>, a, p, 256, s);
+    default: return start(attend_narrow_kernel<DH, 1>, a, p, 256, s);
+  }
 }
 
 }  // namespace
