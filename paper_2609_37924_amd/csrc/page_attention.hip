@@ -22,6 +22,8 @@ namespace tadm {
 namespace {
 
 constexpr float LN2 = 0.6931471805599453f;
+constexpr int VM_DONE = 7 << 4 | 15 << 8;                      // s_waitcnt: no load outstanding
+constexpr int SCHED_MFMA = 0x8, SCHED_LDS_READ = 0x100;        // instruction kinds of a schedule group
 
 struct Args {
   PageLayer p;
@@ -78,13 +80,15 @@ __device__ __forceinline__ int key_of(int i, int grp, int j) {
   return RUN ? 16 * grp + 4 * i + j : 32 * (i >> 1) + 8 * grp + 4 * (i & 1) + j;
 }
 
-// One tile of a column's softmax.  s[i][j]: the score of key_of(i, grp, j), unscaled; on
-// return its probability relative to a reference m (base 2) that moves only when the tile's
-// maximum exceeds it by more than 2^8: until then the probabilities stay below 256 and O
-// needs no rescaling.  Returns the factor for what was summed before.
-template <bool RUN>
-__device__ __forceinline__ float softmax_tile(f32x4 (&s)[4], int keys, int grp, float scale_log2, float& m, float& l) {
-  float mt = -INFINITY;
+// One tile of a strip's softmax, in base 2.  s[i][j]: the score of key_of(i, grp, j), unscaled; on return
+// its probability relative to a reference m of the column, that moves only when a score of the
+// tile exceeds it by more than 2^8: until then the probabilities stay below 256, and neither
+// the sum l nor O need rescaling.  So most tiles need no maximum over the lanes of a column.
+// M_NONE, below every finite score, is the reference before the first.
+constexpr float M_NONE = -3.402823466e38f;
+template <bool RUN, int NB>
+__device__ __forceinline__ void softmax_tile(f32x4 (&s)[4], int keys, int grp, float scale_log2, float& m, float& l,
+                                             f32x4 (&o)[NB]) {
   if (keys < PAGE) {
     asm volatile("" : "+s"(keys));  // the comparisons stay in here
 #pragma unroll
@@ -93,27 +97,29 @@ __device__ __forceinline__ float softmax_tile(f32x4 (&s)[4], int keys, int grp, 
       for (int j = 0; j < 4; ++j)
         if (key_of<RUN>(i, grp, j) >= keys) s[i][j] = -INFINITY;
   }
+  float mt = s[0][0];
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
     for (int j = 0; j < 4; ++j) mt = fmaxf(mt, s[i][j]);
-  mt = fmaxf(mt, xor16(mt));
-  mt = fmaxf(mt, xor32(mt));
-  const float mt2 = mt * scale_log2;
-  const float m_new = mt2 > m + 8.f ? mt2 : m;
-  const float ref = m_new == -INFINITY ? 0.f : m_new;  // no finite score yet: every p is 0
-  const float alpha = __builtin_amdgcn_exp2f(m - ref);
+  if (__builtin_amdgcn_ballot_w64(mt * scale_log2 > m + 8.f)) {
+    mt = fmaxf(mt, xor16(mt));
+    mt = fmaxf(mt, xor32(mt)) * scale_log2;
+    const float m_new = mt > m + 8.f ? mt : m, alpha = __builtin_amdgcn_exp2f(m - m_new);
+    l *= alpha;
+    m = m_new;
+#pragma unroll
+    for (int d = 0; d < NB; ++d) o[d] *= alpha;
+  }
   float ps = 0.f;
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      s[i][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i][j], scale_log2, -ref));
+      s[i][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i][j], scale_log2, -m));
       ps += s[i][j];
     }
-  l = l * alpha + ps;
-  m = m_new;
-  return m == -INFINITY ? 1.f : alpha;
+  l += ps;
 }
 
 // Stores 4 values of column col (head width d0 + [0, 4)) of a strip: part of a split, or the result.
@@ -154,13 +160,12 @@ __device__ __forceinline__ void join_waves(const Args& a, const Block& x, int co
     for (int j = 0; j < 4; ++j) w[(2 + 4 * d + j) * 64] = o[d][j];
   __syncthreads();
   const float* y = xs + lane;
-  float m = -INFINITY, f[NW], sum = 0.f;
+  float m = M_NONE, f[NW], sum = 0.f;
 #pragma unroll
   for (int v = 0; v < NW; ++v) m = fmaxf(m, y[v * NV * 64]);
-  const float ref = m == -INFINITY ? 0.f : m;
 #pragma unroll
   for (int v = 0; v < NW; ++v) {
-    f[v] = __builtin_amdgcn_exp2f(y[v * NV * 64] - ref);
+    f[v] = __builtin_amdgcn_exp2f(y[v * NV * 64] - m);
     sum += y[v * NV * 64 + 64] * f[v];
   }
   const int L = a.r.max_n;
@@ -209,7 +214,7 @@ __global__ __launch_bounds__(256) void attend_f32_kernel(Args a) {
     qx[c] = 16 * c + 4 * grp < dh ? *reinterpret_cast<const f32x4*>(q + 16 * c + 4 * grp) : f32x4{0.f, 0.f, 0.f, 0.f};
     o[c] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  float m_run = -INFINITY, l_run = 0.f;
+  float m_run = M_NONE, l_run = 0.f;
   for (int t = x.t0 + wave; t < x.t1; t += NW) {
     const bool paged = t < x.np;
     const int keys = paged ? min(PAGE, x.len - t * PAGE) : min(PAGE, x.n - (t - x.np) * PAGE);
@@ -240,13 +245,12 @@ __global__ __launch_bounds__(256) void attend_f32_kernel(Args a) {
         for (int e = 0; e < 4; ++e) s[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[e], qx[c][e], s[i], 0, 0, 0);
       }
     }
-    const float alpha = softmax_tile<true>(s, keys, grp, a.scale_log2, m_run, l_run);
+    softmax_tile<true>(s, keys, grp, a.scale_log2, m_run, l_run, o);
     // V^T row 16 d + fr, keys 16 grp + [0, 16); what lies behind the last key is taken as 0, so
     // that p = 0 meets a finite value
 #pragma unroll
     for (int d = 0; d < NB; ++d) {
       const int row = min(16 * d + fr, dh - 1);
-      o[d] *= alpha;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         f32x4 vf = paged ? f32_codes(*reinterpret_cast<const uint32_t*>(codes + PAGE * dh + row * PAGE + 16 * grp + 4 * i), sv)
@@ -324,6 +328,7 @@ __device__ __forceinline__ TileBatch tile_batch(const Args& a, const Block& x, i
       r = TileBatch{page, min(PAGE, x.len - tile * PAGE), sc[0], sc[1]};
     }
   }
+  asm volatile("" : "+v"(r.page), "+v"(r.keys), "+v"(r.sk), "+v"(r.sv));  // waited for here, as in settle()
   return r;
 }
 __device__ __forceinline__ int at_lane(int v, int lane) { return __builtin_amdgcn_readlane(v, lane); }
@@ -369,10 +374,7 @@ __device__ __forceinline__ void window_tile(const Args& a, const Block& x, int w
   bf16x8 p[QS][2];
 #pragma unroll
   for (int u = 0; u < QS; ++u) {
-    const float alpha = softmax_tile<true>(s[u], keys, grp, a.scale_log2, m_run[u], l_run[u]);
-    if (__builtin_amdgcn_ballot_w64(alpha != 1.f))
-#pragma unroll
-      for (int d = 0; d < NB; ++d) o[u][d] *= alpha;
+    softmax_tile<true>(s[u], keys, grp, a.scale_log2, m_run[u], l_run[u], o[u]);
     p_operand(s[u], p[u]);
   }
 #pragma unroll
@@ -408,7 +410,7 @@ __global__ __launch_bounds__(256) void attend_narrow_kernel(Args a) {
 #pragma unroll
   for (int u = 0; u < QS; ++u) {
     q[u] = static_cast<const bf16*>(a.q) + (x.head * ncol + min(x.ct * 16 * QS + 16 * u + fr, ncol - 1)) * DH;
-    m_run[u] = -INFINITY;
+    m_run[u] = M_NONE;
     l_run[u] = 0.f;
 #pragma unroll
     for (int d = 0; d < NB; ++d) o[u][d] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -454,10 +456,7 @@ __global__ __launch_bounds__(256) void attend_narrow_kernel(Args a) {
     bf16x8 p[QS][2];
 #pragma unroll
     for (int u = 0; u < QS; ++u) {
-      const float alpha = softmax_tile<true>(s[u], keys, grp, a.scale_log2, m_run[u], l_run[u]);
-      if (__builtin_amdgcn_ballot_w64(alpha != 1.f))
-#pragma unroll
-        for (int d = 0; d < NB; ++d) o[u][d] *= alpha;
+      softmax_tile<true>(s[u], keys, grp, a.scale_log2, m_run[u], l_run[u], o[u]);
       p_operand(s[u], p[u]);
     }
     // V^T row 16 d + fr, keys 16 grp + [0, 16); what lies behind the last key is taken as 0, so
@@ -497,8 +496,8 @@ __device__ __forceinline__ int swizzle(int row) {
 // 64 keys, which its waves share through LDS.  The groups take turns: while one is at its
 // matrix products (O += V^T P of the tile before, S = K Q^T of this one), the other is at its
 // exponentials, so that each SIMD has a wave for its matrix core and one for its vector unit.
-// A barrier of the whole block ends every such half step.  The next tile's K goes to LDS
-// beside the matrix products and its V, used a step later, beside the exponentials.
+// A barrier of the whole block ends every such half step.  A step's V and the next one's K go to
+// LDS beside the matrix products.
 //
 // The codes of a tile are converted to bf16, scaled, on their way to LDS, once for all waves
 // (with codes in LDS, converted by every wave, the step took 8 % more), the values 0 behind the
@@ -526,7 +525,7 @@ __global__ __launch_bounds__(128 * CW, 2) void attend_wide_kernel(Args a) {
   float m_run[QS], l_run[QS];
 #pragma unroll
   for (int u = 0; u < QS; ++u) {
-    m_run[u] = -INFINITY;
+    m_run[u] = M_NONE;
     l_run[u] = 0.f;
 #pragma unroll
     for (int d = 0; d < NB; ++d) o[u][d] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -540,38 +539,43 @@ __global__ __launch_bounds__(128 * CW, 2) void attend_wide_kernel(Args a) {
   const int v_dst = 2 * BUF + vr * 128 + (gl % 8 ^ swizzle<128>(vr)) * 16;
   auto k_next = [&](int j) { return key_of<false>(KROWS * j >> 4, 0, 0) * DH; };
   TileBatch tb = tile_batch(a, x, x.t0 + kw + 2 * lane, tp);
-  uint2 kc[PER], vc[PER];
-  int page = 0, keys = 0, keys_next = 0;
-  float sk_next = 1.f, sv_next = 1.f;
-  auto load_k = [&](int st) {
-    if (st && (st & 63) == 0) tb = tile_batch(a, x, x.t0 + kw + 2 * (st + lane), tp);
-    page = at_lane(tb.page, st & 63);
-    sk_next = at_lane(tb.sk, st & 63);
-    const uint8_t* c = base + (size_t)page * a.p.page_bytes;
-#pragma unroll
-    for (int j = 0; j < PER; ++j) kc[j] = *reinterpret_cast<const uint2*>(c + k_src + k_next(j));
+  struct Tile {
+    int page, keys;
+    float sk, sv;
   };
-  auto load_v = [&](int st) {
-    keys_next = at_lane(tb.keys, st & 63);
-    sv_next = at_lane(tb.sv, st & 63);
-    const uint8_t* c = base + (size_t)page * a.p.page_bytes;
+  auto tile = [&](int st) {  // of step st; places behind the last tile read page 0, with no keys
+    const int l = st & 63;
+    return Tile{at_lane(tb.page, l), at_lane(tb.keys, l), at_lane(tb.sk, l), at_lane(tb.sv, l)};
+  };
+  uint2 kc[PER], vc[PER];  // codes of the tiles kt and vt
+  Tile kt, vt;
+  auto load_k = [&](const Tile& t) {
+    const uint8_t* c = base + (size_t)t.page * a.p.page_bytes + k_src;
 #pragma unroll
-    for (int j = 0; j < PER; ++j) vc[j] = *reinterpret_cast<const uint2*>(c + SIDE + (gl + GT * j) * 8);
+    for (int j = 0; j < PER; ++j) kc[j] = *reinterpret_cast<const uint2*>(c + k_next(j));
+    kt = t;
+  };
+  auto load_v = [&](const Tile& t) {
+    const uint8_t* c = base + (size_t)t.page * a.p.page_bytes + SIDE;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) vc[j] = *reinterpret_cast<const uint2*>(c + (gl + GT * j) * 8);
+    vt = t;
   };
   auto place_k = [&](int st) {
     char* to = sb + (st & 1) * BUF + k_dst;
 #pragma unroll
     for (int j = 0; j < PER; ++j)
-      *reinterpret_cast<bf16x8*>(to + KROWS * j * 2 * DH) = bf16_codes(kc[j].x, kc[j].y, sk_next);
+      *reinterpret_cast<bf16x8*>(to + KROWS * j * 2 * DH) = bf16_codes(kc[j].x, kc[j].y, kt.sk);
   };
   auto place_v = [&](int st) {
     char* to = sb + (st & 1) * BUF + v_dst;
+    if (vt.keys < PAGE)
 #pragma unroll
-    for (int j = 0; j < PER; ++j) {
-      uint2 w = vc[j];
-      if (keys_next < PAGE) w = uint2{keep_bytes(w.x, keys_next - gl % 8 * 8), keep_bytes(w.y, keys_next - gl % 8 * 8 - 4)};
-      *reinterpret_cast<bf16x8*>(to + VROWS * j * 128) = bf16_codes(w.x, w.y, sv_next);
-    }
+      for (int j = 0; j < PER; ++j)
+        vc[j] = uint2{keep_bytes(vc[j].x, vt.keys - gl % 8 * 8), keep_bytes(vc[j].y, vt.keys - gl % 8 * 8 - 4)};
+#pragma unroll
+    for (int j = 0; j < PER; ++j)
+      *reinterpret_cast<bf16x8*>(to + VROWS * j * 128) = bf16_codes(vc[j].x, vc[j].y, vt.sv);
   };
   // the lane's places in a buffer: K row fr, chunks 4 e + grp; V^T row fr, chunks (8 keys) 4 c + grp
   int kofs[DH / 32], vofs[2];
@@ -580,74 +584,89 @@ __global__ __launch_bounds__(128 * CW, 2) void attend_wide_kernel(Args a) {
 #pragma unroll
   for (int e = 0; e < 2; ++e) vofs[e] = 2 * BUF + fr * 128 + ((4 * e + grp) ^ swizzle<128>(fr)) * 16;
   auto add_pv = [&](int st) {  // O += V^T P of step st
-    const char* sv = sb + (st & 1) * BUF;
+    const char* from = sb + (st & 1) * BUF;
 #pragma unroll
-    for (int d = 0; d < NB; ++d)
+    for (int c = 0; c < 2; ++c)  // a product's sum is not taken up again before NB QS others
 #pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        const bf16x8 vf = *reinterpret_cast<const bf16x8*>(sv + d * 16 * 128 + vofs[c]);
+      for (int d = 0; d < NB; ++d) {
+        const bf16x8 vf = *reinterpret_cast<const bf16x8*>(from + d * 16 * 128 + vofs[c]);
 #pragma unroll
         for (int u = 0; u < QS; ++u) o[u][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, p[u][c], o[u][d], 0, 0, 0);
       }
+  };
+  auto score = [&](int st) {  // S = K Q^T of step st
+    const char* from = sb + (st & 1) * BUF;
+#pragma unroll
+    for (int e = 0; e < DH / 32; ++e)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const bf16x8 k = *reinterpret_cast<const bf16x8*>(from + i * 32 * DH + kofs[e]);
+#pragma unroll
+        for (int u = 0; u < QS; ++u)
+          s[u][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, qs[u].op[e], e ? s[u][i] : f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+      }
+  };
+  int keys = 0;
+  // Beside the products of step st: the next K and this V go to LDS, those after them to registers.
+  auto move = [&](int st, const Tile& after) {
+    const Tile next = kt;
+    place_k(st + 1);
+    load_k(after);
+    place_v(st);
+    keys = vt.keys;
+    load_v(next);
+  };
+  auto soften = [&]() {  // P of the step
+#pragma unroll
+    for (int u = 0; u < QS; ++u) {
+      softmax_tile<false>(s[u], keys, grp, a.scale_log2, m_run[u], l_run[u], o[u]);
+      p_operand(s[u], p[u]);
+    }
   };
   const bf16* q[QS];
 #pragma unroll
   for (int u = 0; u < QS; ++u)
     q[u] = static_cast<const bf16*>(a.q) + (x.head * ncol + min(col0 + 16 * u + fr, ncol - 1)) * DH;
   if (steps) {
-    load_k(0);
-    load_v(0);
+    load_k(tile(0));
+    load_v(tile(0));
 #pragma unroll
     for (int u = 0; u < QS; ++u) qs[u] = load_query<DH, false>(q[u], grp);
     place_k(0);
-    place_v(0);
-    keys = keys_next;
-    if (steps > 1) {
-      load_k(1);
-      load_v(1);
-    }
-  }
+    load_k(tile(1));
 #pragma unroll
-  for (int u = 0; u < QS; ++u) settle<DH>(qs[u]);
-  if (kw) __syncthreads();  // the second group is half a step behind
-  for (int st = 0; st < steps; ++st) {
-    __syncthreads();  // the group's K of this step and V of the one before are in LDS
-    if (st + 1 < steps) {
-      place_k(st + 1);
-      if (st + 2 < steps) load_k(st + 2);
-    }
-    if (st) add_pv(st - 1);
-    const char* sk = sb + (st & 1) * BUF;
+    for (int u = 0; u < QS; ++u) settle<DH>(qs[u]);
+    __builtin_amdgcn_s_waitcnt(VM_DONE);  // so that the waits in the loop count its own loads alone
+    if (kw) __syncthreads();              // the second group is half a step behind
+    __syncthreads();
+    move(0, tile(2));
+    score(0);
+    __syncthreads();
+    soften();
+    for (int st = 1; st < steps; ++st) {
+      if (((st + 2) & 63) == 0) tb = tile_batch(a, x, x.t0 + kw + 2 * (st + 2 + lane), tp);
+      const Tile after = tile(st + 2);
+      __syncthreads();  // the group's K of this step and V of the one before are in LDS
+      move(st, after);
+      add_pv(st - 1);
+      score(st);
+      // reads of LDS run 8 ahead of the products that take them: left to itself the compiler has
+      // two in flight, and waits out their latency 16 times a step
+      constexpr int READS = 2 * NB + DH / 8, AHEAD = 8;
+      __builtin_amdgcn_sched_group_barrier(SCHED_LDS_READ, AHEAD, 0);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-#pragma unroll
-      for (int u = 0; u < QS; ++u) s[u][i] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int e = 0; e < DH / 32; ++e) {
-        const bf16x8 k = *reinterpret_cast<const bf16x8*>(sk + i * 32 * DH + kofs[e]);
-#pragma unroll
-        for (int u = 0; u < QS; ++u) s[u][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, qs[u].op[e], s[u][i], 0, 0, 0);
+      for (int r = AHEAD; r < READS; ++r) {
+        __builtin_amdgcn_sched_group_barrier(SCHED_MFMA, QS, 0);
+        __builtin_amdgcn_sched_group_barrier(SCHED_LDS_READ, 1, 0);
       }
+      __builtin_amdgcn_sched_group_barrier(SCHED_MFMA, QS * AHEAD, 0);
+      __syncthreads();  // the group is done with V of the step before
+      soften();
     }
-    __syncthreads();  // the group is done with V of the step before
-    const int keys_now = keys;
-    if (st + 1 < steps) {
-      place_v(st + 1);
-      keys = keys_next;
-      if (st + 2 < steps) load_v(st + 2);
-    }
-#pragma unroll
-    for (int u = 0; u < QS; ++u) {
-      const float alpha = softmax_tile<false>(s[u], keys_now, grp, a.scale_log2, m_run[u], l_run[u]);
-      if (__builtin_amdgcn_ballot_w64(alpha != 1.f))
-#pragma unroll
-        for (int d = 0; d < NB; ++d) o[u][d] *= alpha;
-      p_operand(s[u], p[u]);
-    }
+    __syncthreads();
+    add_pv(steps - 1);
+    if (!kw) __syncthreads();
   }
-  __syncthreads();
-  if (steps) add_pv(steps - 1);
-  if (!kw) __syncthreads();
   for (int t = max(x.t0, x.np); t < x.t1; ++t)
     if (((t - x.t0) & 1) == kw) window_tile<DH, QS>(a, x, t - x.np, q, o, m_run, l_run);
   // the second group joins the first, a strip at a time
@@ -667,8 +686,8 @@ __global__ __launch_bounds__(128 * CW, 2) void attend_wide_kernel(Args a) {
     }
     __syncthreads();
     if (kw == 0) {
-      const float m = fmaxf(m_run[u], w[0]), ref = m == -INFINITY ? 0.f : m;
-      const float f0 = __builtin_amdgcn_exp2f(m_run[u] - ref), f1 = __builtin_amdgcn_exp2f(w[0] - ref);
+      const float m = fmaxf(m_run[u], w[0]);
+      const float f0 = __builtin_amdgcn_exp2f(m_run[u] - m), f1 = __builtin_amdgcn_exp2f(w[0] - m);
       const float l = l_run[u] * f0 + w[64] * f1;
       const int col = col0 + 16 * u + fr;
       if (col < ncol && col % a.r.max_n < x.n) {
@@ -698,15 +717,14 @@ __global__ __launch_bounds__(256) void join_kernel(Args a) {
   const int b = (int)(col_id / ncol / a.p.Hkv), h = (int)(col_id / ncol % a.p.Hkv);
   if (j >= row_new(a.r, b)) return;
   const float* ml = part_ml(a, col_id, 0);
-  float m = -INFINITY;
+  float m = M_NONE;
   for (int s = lane; s < a.S; s += 64) m = fmaxf(m, ml[2 * s]);
   m = wave_max(m);
-  const float ref = m == -INFINITY ? 0.f : m;
   const float* po = part_o(a, col_id, 0) + 4 * i;
   float r[4] = {0.f, 0.f, 0.f, 0.f}, sum = 0.f;
 #pragma unroll 4
   for (int s = g8; s < a.S; s += 8) {
-    const float f = __builtin_amdgcn_exp2f(ml[2 * s] - ref);
+    const float f = __builtin_amdgcn_exp2f(ml[2 * s] - m);
     sum += ml[2 * s + 1] * f;
     if (4 * i < dh) {
       const f32x4 v = *reinterpret_cast<const f32x4*>(po + (size_t)s * dh);
