@@ -328,8 +328,11 @@ __device__ __forceinline__ TileBatch tile_batch(const Args& a, const Block& x, i
       r = TileBatch{page, min(PAGE, x.len - tile * PAGE), sc[0], sc[1]};
     }
   }
-  asm volatile("" : "+v"(r.page), "+v"(r.keys), "+v"(r.sk), "+v"(r.sv));  // waited for here, as in settle()
   return r;
+}
+// Waits for a batch's loads here, as for a query's.
+__device__ __forceinline__ void settle(TileBatch& b) {
+  asm volatile("" : "+v"(b.page), "+v"(b.keys), "+v"(b.sk), "+v"(b.sv));
 }
 __device__ __forceinline__ int at_lane(int v, int lane) { return __builtin_amdgcn_readlane(v, lane); }
 __device__ __forceinline__ float at_lane(float v, int lane) {
@@ -391,11 +394,11 @@ __device__ __forceinline__ void window_tile(const Args& a, const Block& x, int w
     }
 }
 
-// Few columns: four waves on the same 16 QS columns, each taking every fourth tile straight from
+// Few columns: NW waves on the same 16 QS columns, each taking every NW-th tile straight from
 // memory into registers; the codes of the next tile are on their way while one is computed.
-template <int DH, int QS>
-__global__ __launch_bounds__(256) void attend_narrow_kernel(Args a) {
-  constexpr int NW = 4, NB = DH / 16;
+template <int DH, int QS, int NW>
+__global__ __launch_bounds__(64 * NW) void attend_narrow_kernel(Args a) {
+  constexpr int NB = DH / 16;
   __shared__ float xs[NW * (2 + 4 * NB) * 64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), grp = lane >> 4,
             fr = lane & 15;
@@ -433,48 +436,53 @@ __global__ __launch_bounds__(256) void attend_narrow_kernel(Args a) {
     for (int d = 0; d < NB; ++d) vc[d] = *reinterpret_cast<const uint4*>(c + 16 * d * PAGE);
   };
   if (steps) {
-    const int page = at_lane(tb.page, 0);
-    load_k(page);
-    load_v(page);
-  }
 #pragma unroll
-  for (int u = 0; u < QS; ++u) qs[u] = load_query<DH, true>(q[u], grp);
+    for (int u = 0; u < QS; ++u) qs[u] = load_query<DH, true>(q[u], grp);
+    const int first_page = at_lane(tb.page, 0);
+    load_k(first_page);
+    load_v(first_page);
 #pragma unroll
-  for (int u = 0; u < QS; ++u) settle<DH>(qs[u]);
-  for (int st = 0; st < steps; ++st) {
-    const int keys = at_lane(tb.keys, st & 63);
-    const float sk = at_lane(tb.sk, st & 63), sv = at_lane(tb.sv, st & 63);
-    f32x4 s[QS][4];
+    for (int u = 0; u < QS; ++u) settle<DH>(qs[u]);
+    settle(tb);
+    __builtin_amdgcn_s_waitcnt(VM_DONE);  // so that the waits in the loop count its own loads alone
+    for (int st = 0; st < steps; ++st) {
+      const int keys = at_lane(tb.keys, st & 63);
+      const float sk = at_lane(tb.sk, st & 63), sv = at_lane(tb.sv, st & 63);
+      if (((st + 1) & 63) == 0) {
+        tb = tile_batch(a, x, first + NW * (st + 1 + lane), tp);
+        settle(tb);
+      }
+      const int page = at_lane(tb.page, (st + 1) & 63);  // behind the last tile: page 0
+      f32x4 s[QS][4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) scores<DH, QS>(kc[i], sk, qs, i, s);
-    int page = 0;
-    if (st + 1 < steps) {
-      if (((st + 1) & 63) == 0) tb = tile_batch(a, x, first + NW * (st + 1 + lane), tp);
-      page = at_lane(tb.page, (st + 1) & 63);
+      for (int i = 0; i < 4; ++i) scores<DH, QS>(kc[i], sk, qs, i, s);
       load_k(page);
-    }
-    bf16x8 p[QS][2];
+      bf16x8 p[QS][2];
 #pragma unroll
-    for (int u = 0; u < QS; ++u) {
-      softmax_tile<true>(s[u], keys, grp, a.scale_log2, m_run[u], l_run[u], o[u]);
-      p_operand(s[u], p[u]);
-    }
-    // V^T row 16 d + fr, keys 16 grp + [0, 16); what lies behind the last key is taken as 0, so
-    // that p = 0 meets a finite value
-#pragma unroll
-    for (int d = 0; d < NB; ++d) {
-      uint32_t w[4] = {vc[d].x, vc[d].y, vc[d].z, vc[d].w};
+      for (int u = 0; u < QS; ++u) {
+        softmax_tile<true>(s[u], keys, grp, a.scale_log2, m_run[u], l_run[u], o[u]);
+        p_operand(s[u], p[u]);
+      }
+      // V^T row 16 d + fr, keys 16 grp + [0, 16); what lies behind the last key is taken as 0, so
+      // that p = 0 meets a finite value
       if (keys < PAGE)
 #pragma unroll
-        for (int c = 0; c < 4; ++c) w[c] = keep_bytes(w[c], keys - 16 * grp - 4 * c);
+        for (int d = 0; d < NB; ++d) {
+          vc[d].x = keep_bytes(vc[d].x, keys - 16 * grp);
+          vc[d].y = keep_bytes(vc[d].y, keys - 16 * grp - 4);
+          vc[d].z = keep_bytes(vc[d].z, keys - 16 * grp - 8);
+          vc[d].w = keep_bytes(vc[d].w, keys - 16 * grp - 12);
+        }
 #pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        const bf16x8 vf = bf16_codes(w[2 * c], w[2 * c + 1], sv);
+      for (int d = 0; d < NB; ++d)
 #pragma unroll
-        for (int u = 0; u < QS; ++u) o[u][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, p[u][c], o[u][d], 0, 0, 0);
-      }
+        for (int c = 0; c < 2; ++c) {
+          const bf16x8 vf = c ? bf16_codes(vc[d].z, vc[d].w, sv) : bf16_codes(vc[d].x, vc[d].y, sv);
+#pragma unroll
+          for (int u = 0; u < QS; ++u) o[u][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, p[u][c], o[u][d], 0, 0, 0);
+        }
+      load_v(page);
     }
-    if (st + 1 < steps) load_v(page);
   }
   for (int t = max(x.t0, x.np); t < x.t1; ++t)
     if ((t - x.t0) % NW == wave) window_tile<DH, QS>(a, x, t - x.np, q, o, m_run, l_run);
@@ -628,10 +636,13 @@ __global__ __launch_bounds__(128 * CW, 2) void attend_wide_kernel(Args a) {
   for (int u = 0; u < QS; ++u)
     q[u] = static_cast<const bf16*>(a.q) + (x.head * ncol + min(col0 + 16 * u + fr, ncol - 1)) * DH;
   if (steps) {
-    load_k(tile(0));
-    load_v(tile(0));
 #pragma unroll
     for (int u = 0; u < QS; ++u) qs[u] = load_query<DH, false>(q[u], grp);
+    const int page0 = at_lane(tb.page, 0);
+    load_k(Tile{page0});  // before the scales are there
+    load_v(Tile{page0});
+    settle(tb);
+    kt = vt = tile(0);
     place_k(0);
     load_k(tile(1));
 #pragma unroll
@@ -644,7 +655,10 @@ __global__ __launch_bounds__(128 * CW, 2) void attend_wide_kernel(Args a) {
     __syncthreads();
     soften();
     for (int st = 1; st < steps; ++st) {
-      if (((st + 2) & 63) == 0) tb = tile_batch(a, x, x.t0 + kw + 2 * (st + 2 + lane), tp);
+      if (((st + 2) & 63) == 0) {
+        tb = tile_batch(a, x, x.t0 + kw + 2 * (st + 2 + lane), tp);
+        settle(tb);
+      }
       const Tile after = tile(st + 2);
       __syncthreads();  // the group's K of this step and V of the one before are in LDS
       move(st, after);
@@ -749,6 +763,8 @@ __global__ __launch_bounds__(256) void join_kernel(Args a) {
   if (threadIdx.x == 0 && a.lse) a.lse[col_id] = sum == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * LN2;
 }
 
+constexpr int NARROW_WAVES = 8;  // of a block with few columns
+
 // Which kernel a call takes: columns of a block, tiles that its waves work on at once, splits.
 struct Plan {
   int width, waves, S;
@@ -758,7 +774,7 @@ Plan plan(DType dt, int B, int H, int Hkv, int L, int max_len) {
   const int ncol = H / Hkv * L;
   const int tiles = (max_len + PAGE - 1) / PAGE + (L + PAGE - 1) / PAGE;
   auto blocks = [&](int width) { return (long)B * Hkv * ((ncol + width - 1) / width); };
-  Plan p{16, 4, 1};
+  Plan p{16, dt == BF16 ? NARROW_WAVES : 4, 1};
   const bool wide = dt == BF16 && ncol > 32;
   if (wide) {
     p = Plan{blocks(128) < 256 ? 64 : 128, 2, 1};
@@ -766,7 +782,7 @@ Plan plan(DType dt, int B, int H, int Hkv, int L, int max_len) {
     p.width = 32;
   }
   const long n = blocks(p.width), most = (tiles + 4 * p.waves - 1) / (4 * p.waves);  // four tiles per wave at least
-  long S = (wide ? 256 : 768) / n;
+  long S = 256 / n;                                                                  // a block per CU
   S = S < most ? S : most;
   p.S = S < 1 ? 1 : (int)S;
   return p;
@@ -783,8 +799,8 @@ void start_bf16(const Args& a, const Plan& p, hipStream_t s) {
   switch (p.width) {
     case 128: return start(attend_wide_kernel<DH, 2, 4>, a, p, 512, s);
     case 64: return start(attend_wide_kernel<DH, 1, 4>, a, p, 512, s);
-    case 32: return start(attend_narrow_kernel<DH, 2>, a, p, 256, s);
-    default: return start(attend_narrow_kernel<DH, 1>, a, p, 256, s);
+    case 32: return start(attend_narrow_kernel<DH, 2, NARROW_WAVES>, a, p, 64 * NARROW_WAVES, s);
+    default: return start(attend_narrow_kernel<DH, 1, NARROW_WAVES>, a, p, 64 * NARROW_WAVES, s);
   }
 }
 
