@@ -374,6 +374,15 @@ __device__ __forceinline__ void window_tile(const Args& a, const Block& x, int w
       for (int u = 0; u < QS; ++u) s[u][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[u], s[u][i], 0, 0, 0);
     }
   }
+  // one strip: the values are on their way while the scores wait for theirs
+  constexpr bool AHEAD = QS == 1;
+  bf16x8 v[AHEAD ? NB : 1][2];
+  if constexpr (AHEAD)
+#pragma unroll
+    for (int d = 0; d < NB; ++d)
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+        v[d][c] = *reinterpret_cast<const bf16x8*>(vw + (size_t)(16 * d + fr) * a.cap + 16 * grp + 8 * c);
   bf16x8 p[QS][2];
 #pragma unroll
   for (int u = 0; u < QS; ++u) {
@@ -384,7 +393,8 @@ __device__ __forceinline__ void window_tile(const Args& a, const Block& x, int w
   for (int d = 0; d < NB; ++d)
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
-      bf16x8 vf = *reinterpret_cast<const bf16x8*>(vw + (size_t)(16 * d + fr) * a.cap + 16 * grp + 8 * c);
+      bf16x8 vf = v[AHEAD ? d : 0][c];
+      if (!AHEAD) vf = *reinterpret_cast<const bf16x8*>(vw + (size_t)(16 * d + fr) * a.cap + 16 * grp + 8 * c);
       if (keys < PAGE)
 #pragma unroll
         for (int j = 0; j < 8; ++j)
@@ -719,48 +729,68 @@ __global__ __launch_bounds__(128 * CW, 2) void attend_wide_kernel(Args a) {
   }
 }
 
-// Joins the splits of a column, one block each: eight groups of 32 lanes take every eighth
-// split, four values of the head width a lane, and are summed in order.
-template <class T>
+// Joins the splits of a column: GROUPS groups of 32 lanes, four values of the head width a lane, take every
+// GROUPS-th split and are summed in order; a block has eight groups.
+template <class T, int GROUPS>
 __global__ __launch_bounds__(256) void join_kernel(Args a) {
-  __shared__ float xs[8][132];
-  const int lane = threadIdx.x & 63, g8 = threadIdx.x >> 5, i = threadIdx.x & 31;
+  __shared__ float xs[GROUPS > 1 ? GROUPS : 1][132];
+  const int i = threadIdx.x & 31, g8 = threadIdx.x / 32 % GROUPS;
   const int L = a.r.max_n, ncol = a.G * L, dh = a.p.dh;
-  const size_t col_id = blockIdx.x;
+  const size_t cols = (size_t)a.r.B * a.p.Hkv * ncol, id = (size_t)blockIdx.x * (8 / GROUPS) + threadIdx.x / (32 * GROUPS);
+  const size_t col_id = id < cols ? id : cols - 1;
   const int col = (int)(col_id % ncol), g = col / L, j = col % L;
   const int b = (int)(col_id / ncol / a.p.Hkv), h = (int)(col_id / ncol % a.p.Hkv);
-  if (j >= row_new(a.r, b)) return;
+  const bool mine = id < cols && j < row_new(a.r, b);
+  if (GROUPS == 8 && !mine) return;  // the whole block
   const float* ml = part_ml(a, col_id, 0);
   float m = M_NONE;
-  for (int s = lane; s < a.S; s += 64) m = fmaxf(m, ml[2 * s]);
-  m = wave_max(m);
+  if (mine)
+    for (int s = i; s < a.S; s += 32) m = fmaxf(m, ml[2 * s]);
+  m = row16_max(m);
+  m = fmaxf(m, xor16(m));
   const float* po = part_o(a, col_id, 0) + 4 * i;
   float r[4] = {0.f, 0.f, 0.f, 0.f}, sum = 0.f;
+  if (mine)
 #pragma unroll 4
-  for (int s = g8; s < a.S; s += 8) {
-    const float f = __builtin_amdgcn_exp2f(ml[2 * s] - m);
-    sum += ml[2 * s + 1] * f;
-    if (4 * i < dh) {
-      const f32x4 v = *reinterpret_cast<const f32x4*>(po + (size_t)s * dh);
+    for (int s = g8; s < a.S; s += GROUPS) {
+      const float f = __builtin_amdgcn_exp2f(ml[2 * s] - m);
+      sum += ml[2 * s + 1] * f;
+      if (4 * i < dh) {
+        const f32x4 v = *reinterpret_cast<const f32x4*>(po + (size_t)s * dh);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) r[e] += v[e] * f;
+        for (int e = 0; e < 4; ++e) r[e] += v[e] * f;
+      }
+    }
+  if constexpr (GROUPS > 1) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) xs[g8][4 * i + e] = r[e];
+    if (i == 0) xs[g8][128] = sum;
+    __syncthreads();
+    if (threadIdx.x >= 32) return;
+    sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) r[e] = 0.f;
+#pragma unroll
+    for (int v = 0; v < GROUPS; ++v) {
+      sum += xs[v][128];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) r[e] += xs[v][4 * i + e];
     }
   }
-#pragma unroll
-  for (int e = 0; e < 4; ++e) xs[g8][4 * i + e] = r[e];
-  if (i == 0) xs[g8][128] = sum;
-  __syncthreads();
-  sum = 0.f;
-#pragma unroll
-  for (int v = 0; v < 8; ++v) sum += xs[v][128];
+  if (!mine) return;
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
-  if (threadIdx.x < dh) {
-    float o = 0.f;
-#pragma unroll
-    for (int v = 0; v < 8; ++v) o += xs[v][threadIdx.x];
-    static_cast<T*>(a.o)[(((size_t)b * L + j) * a.p.Hkv * a.G + h * a.G + g) * dh + threadIdx.x] = from_f32<T>(o * inv);
-  }
-  if (threadIdx.x == 0 && a.lse) a.lse[col_id] = sum == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * LN2;
+  T* out = static_cast<T*>(a.o) + (((size_t)b * L + j) * a.p.Hkv * a.G + h * a.G + g) * dh;
+  if (4 * i < dh) store4(out + 4 * i, r[0] * inv, r[1] * inv, r[2] * inv, r[3] * inv);
+  if (i == 0 && a.lse) a.lse[col_id] = sum == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * LN2;
+}
+// Eight groups a column from 9 splits on, one below.
+template <class T>
+void start_join(const Args& a, hipStream_t s) {
+  const size_t cols = (size_t)a.r.B * a.p.Hkv * a.G * a.r.max_n;
+  if (a.S > 8)
+    hipLaunchKernelGGL((join_kernel<T, 8>), dim3((unsigned)cols), dim3(256), 0, s, a);
+  else
+    hipLaunchKernelGGL((join_kernel<T, 1>), dim3((unsigned)((cols + 7) / 8)), dim3(256), 0, s, a);
 }
 
 constexpr int NARROW_WAVES = 8;  // of a block with few columns
@@ -837,11 +867,10 @@ hipError_t page_attend(DType dt, const PageAttend& c, hipStream_t s) {
     }
   }
   if (pl.S > 1) {
-    const dim3 cols((unsigned)((size_t)a.r.B * a.p.Hkv * a.G * a.r.max_n));
     if (dt == BF16)
-      hipLaunchKernelGGL(join_kernel<bf16>, cols, dim3(256), 0, s, a);
+      start_join<bf16>(a, s);
     else
-      hipLaunchKernelGGL(join_kernel<float>, cols, dim3(256), 0, s, a);
+      start_join<float>(a, s);
   }
   return hipGetLastError();
 }
