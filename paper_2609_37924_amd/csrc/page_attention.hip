@@ -783,11 +783,13 @@ __global__ __launch_bounds__(256) void join_kernel(Args a) {
   if (4 * i < dh) store4(out + 4 * i, r[0] * inv, r[1] * inv, r[2] * inv, r[3] * inv);
   if (i == 0 && a.lse) a.lse[col_id] = sum == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * LN2;
 }
-// Eight groups a column from 9 splits on, one below.
+// Eight groups a column for many splits or few columns, where the loads of one group in a row are what takes
+// time (16 columns of 8 splits: 19.4 us with one group, 16.5 with eight, the attention included); else one,
+// which needs an eighth of the blocks (16 384 columns of 2 splits: 59 us with eight, 40 with one).
 template <class T>
 void start_join(const Args& a, hipStream_t s) {
   const size_t cols = (size_t)a.r.B * a.p.Hkv * a.G * a.r.max_n;
-  if (a.S > 8)
+  if (a.S > 8 || cols <= 2048)
     hipLaunchKernelGGL((join_kernel<T, 8>), dim3((unsigned)cols), dim3(256), 0, s, a);
   else
     hipLaunchKernelGGL((join_kernel<T, 1>), dim3((unsigned)((cols + 7) / 8)), dim3(256), 0, s, a);
@@ -795,24 +797,35 @@ void start_join(const Args& a, hipStream_t s) {
 
 constexpr int NARROW_WAVES = 8;  // of a block with few columns
 
-// Which kernel a call takes: columns of a block, tiles that its waves work on at once, splits.
+// Which kernel a call takes: columns of a block, and splits of the key axis.
 struct Plan {
-  int width, waves, S;
+  int width, S;
 };
 
-Plan plan(DType dt, int B, int H, int Hkv, int L, int max_len) {
+// Measured on one MI355X, in us a call with everything around it:
+//  - Blocks of 128 columns, unless those of 64 are needed to give every CU one (2 rows x 256 tokens over 1 000
+//    positions, 32/16 heads x 128: 34 with 64 columns, 43 with 128; 4 rows: 66 and 44).
+//  - At most a block per CU in all: 16 tokens over 8 192 positions (256 blocks) take 81, and 95 in two splits;
+//    1 token over 131 071 31 in 64 splits of 4 blocks, 34 in 32, and 46 in 128.
+//  - Few columns: a split has two tiles of 128 or four of 64 elements a key, from 9 and 25 tiles on (1 token,
+//    16/4 heads x 128, over 8 000 positions: 49 in one split, 11.7 in 32; over 300, 9.0 in one and 10.6 in two;
+//    12 heads x 64 over 1 000 positions, 17 tiles: 8.0 in one, 9.3 in 16).
+//  - Many: a split has eight tiles, four steps of its two groups (64 tokens, 32/16 heads x 128, over 4 000
+//    positions: 53 in one split, 26 in 8; 12 heads x 64, 2 rows over 500: 10.5 in one, 12.7 in two).
+Plan plan(DType dt, int B, int H, int Hkv, int dh, int L, int max_len) {
   const int ncol = H / Hkv * L;
   const int tiles = (max_len + PAGE - 1) / PAGE + (L + PAGE - 1) / PAGE;
   auto blocks = [&](int width) { return (long)B * Hkv * ((ncol + width - 1) / width); };
-  Plan p{16, dt == BF16 ? NARROW_WAVES : 4, 1};
-  const bool wide = dt == BF16 && ncol > 32;
-  if (wide) {
-    p = Plan{blocks(128) < 256 ? 64 : 128, 2, 1};
-  } else if (dt == BF16 && ncol > 16) {
-    p.width = 32;
+  Plan p{16, 1};
+  long most = tiles > 8 ? tiles / 4 : 1;  // float32
+  if (dt == BF16 && ncol > 32) {
+    p.width = blocks(128) < 256 ? 64 : 128;
+    most = tiles / 8;
+  } else if (dt == BF16) {
+    p.width = ncol > 16 ? 32 : 16;
+    most = dh > 64 ? (tiles > 8 ? tiles / 2 : 1) : (tiles > 24 ? tiles / 4 : 1);
   }
-  const long n = blocks(p.width), most = (tiles + 4 * p.waves - 1) / (4 * p.waves);  // four tiles per wave at least
-  long S = 256 / n;                                                                  // a block per CU
+  long S = 256 / blocks(p.width);
   S = S < most ? S : most;
   p.S = S < 1 ? 1 : (int)S;
   return p;
@@ -837,13 +850,13 @@ void start_bf16(const Args& a, const Plan& p, hipStream_t s) {
 }  // namespace
 
 size_t page_attend_work(DType dt, int B, int H, int Hkv, int dh, int L, int max_len) {
-  const Plan pl = plan(dt, B, H, Hkv, L, max_len);
+  const Plan pl = plan(dt, B, H, Hkv, dh, L, max_len);
   return pl.S > 1 ? (size_t)B * H * L * pl.S * (dh + 2) * sizeof(float) : 0;
 }
 
 hipError_t page_attend(DType dt, const PageAttend& c, hipStream_t s) {
   const int dh = c.p.dh;
-  const Plan pl = plan(dt, c.r.B, c.H, c.p.Hkv, c.r.max_n, c.r.max_len);
+  const Plan pl = plan(dt, c.r.B, c.H, c.p.Hkv, dh, c.r.max_n, c.r.max_len);
   Args a{c.p, c.r, c.q, c.k, c.vt, c.o, c.lse, static_cast<float*>(c.work), c.H / c.p.Hkv, c.cap, pl.S,
          1.4426950408889634f / sqrtf((float)dh)};
   if (dt == BF16) {
