@@ -190,8 +190,9 @@ typedef struct {
  * written to it, and its positions take no part in attention.  The row holds
  * positions [0, len_b): len_b = len for every row, or with len_dev len_dev[b] cut to
  * [0, len].  Its window has n_b new tokens: n, or n_dev[b] cut to [0, n] (n is an
- * argument of each call).  Lengths on the device are not read on the host, so a captured
- * call serves any lengths within len and n. */
+ * argument of each call; B * n, times n_heads in attention, is at most 2^26).  Lengths on
+ * the device are not read on the host, so a captured call serves any lengths within len
+ * and n.  What a call writes may not overlap anything else that it reads or writes. */
 typedef struct {
   const int32_t* table_dev; /* int32 [B, max_pages] */
   const int32_t* len_dev;   /* nullable int32 [B] */
@@ -254,7 +255,8 @@ int32_t tadm_pool_size(const tadm_pool* pool);
 int32_t tadm_pool_free_pages(const tadm_pool* pool);
 /* The pool's arrays for the operators above; valid until tadm_pool_resize. */
 tadm_status tadm_pool_pages(const tadm_pool* pool, tadm_pages* out);
-/* Moves the held pages to the lowest ids, in the contexts' tables too (enqueued like any work). */
+/* Moves the held pages to the lowest ids, in the contexts' tables too (enqueued like any work; not under
+ * graph capture: TADM_ERR_STATE). */
 tadm_status tadm_pool_compact(tadm_pool* pool);
 /* Compacts, then gives the pool n_pages pages (at least those held, TADM_ERR_INVALID otherwise) in a
  * new allocation.  Waits for the device; captured work on the pool is void. */
@@ -264,7 +266,10 @@ tadm_status tadm_pool_resize(tadm_pool* pool, int32_t n_pages);
  * takes it.  Committed positions are held in 8 bits; the active window's K, V stay in
  * the model dtype.  Pages are taken as positions are appended: tadm_context_append
  * returns TADM_ERR_OOM, without side effects, when the pool has too few.  reset and
- * destroy give them back.  tadm_context_read returns the pages' values. */
+ * destroy give them back.  tadm_context_read returns the pages' values.  Passes over the
+ * context may be captured and find its pages where they are at each replay, at the length
+ * of the capture; tadm_context_append may not (TADM_ERR_STATE), since a replay would write
+ * to pages that others may hold by then. */
 tadm_status tadm_context_create_pooled(tadm_model* m, tadm_pool* pool, int32_t B, int32_t max_ctx,
                                        tadm_context** out);
 /* A new context of B rows with the length and capacity of `src`, row b holding what row rows[b] (host

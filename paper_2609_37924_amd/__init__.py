@@ -248,7 +248,7 @@ def page_set(data, scale):
     n_pages, n_layers, heads, two, width = data.shape
     if two != 2 or width % PAGE or tuple(scale.shape) != (n_pages, n_layers, heads, 2):
         raise ValueError(f"pages of shape {tuple(data.shape)} with scales of shape {tuple(scale.shape)}")
-    if data.element_size() != 1 or scale.element_size() != 4:
+    if data.element_size() != 1 or not scale.is_floating_point() or scale.element_size() != 4:
         raise ValueError("pages hold 8-bit codes and float32 scales")
     if not (data.is_contiguous() and scale.is_contiguous()):
         raise ValueError("pages and scales must be contiguous")
@@ -261,6 +261,12 @@ def page_rows(table, length, len_dev=None, n_dev=None):
     positions of every row, or the most of any row when the device tensor len_dev (int32
     [B]) has each row's; n_dev (int32 [B]) the tokens of each row's window.  The caller
     keeps the tensors alive."""
+    if table.dim() != 2:
+        raise ValueError(f"a table of shape {tuple(table.shape)}")
+    for name, t, shape in (("table", table, tuple(table.shape)), ("len_dev", len_dev, (table.shape[0],)),
+                           ("n_dev", n_dev, (table.shape[0],))):
+        if t is not None and (str(t.dtype) != "torch.int32" or tuple(t.shape) != shape or not t.is_contiguous()):
+            raise ValueError(f"{name} must be contiguous int32 of shape {shape}")
     return tadm_page_rows(table_dev=ptr(table), len_dev=ptr(len_dev), n_dev=ptr(n_dev), B=table.shape[0],
                           max_pages=table.shape[1], len=length)
 

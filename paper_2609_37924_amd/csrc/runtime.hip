@@ -1209,9 +1209,19 @@ static void context_drop(tadm_context* x, int len) {
   if (x->pool) x->pool->book.drop(x->table, (len + PAGE - 1) / PAGE);
 }
 
+// Pages are handed out by the host as calls are enqueued; a replay would hand out those of the capture
+// again, whoever holds them by then.
+static tadm_status check_no_capture(const tadm_model* m, const char* what) {
+  if (!m->stream) return TADM_OK;  // the null stream is never captured
+  hipStreamCaptureStatus st;
+  HIPCHK(hipStreamIsCapturing(m->stream, &st));
+  return st == hipStreamCaptureStatusNone ? TADM_OK : fail(TADM_ERR_STATE, "%s cannot be captured", what);
+}
+
 // Gives every row of a pooled context pages of its own for the positions [len, len + n).
 // Nothing has changed when it fails for want of pages.
 static tadm_status pages_take(tadm_context* x, int n) {
+  TRY(check_no_capture(x->model, "appending to a pooled context"));
   tadm_pool* p = x->pool;
   PageMoves mv;
   try {
@@ -1340,6 +1350,15 @@ static tadm_status check_rows(const tadm_page_rows* r) {
   return TADM_OK;
 }
 
+// A window of n tokens and n queries of each for each of `heads` heads (0: not known yet): a launch's threads and
+// the positions of a row stay below 2^31.
+static tadm_status check_window_size(const tadm_page_rows* rows, int n, int heads) {
+  if (n < 1 || n > (1 << 26)) return fail(TADM_ERR_INVALID, "n=%d outside [1, 2^26]", n);
+  if ((long)rows->B * n > (1 << 26) / std::max(heads, 1))
+    return fail(TADM_ERR_INVALID, "%d rows of %d queries: too many in one call, which takes 2^26", rows->B, n);
+  return TADM_OK;
+}
+
 // A window's K, V^T arrays with n tokens.
 static tadm_status check_window_kv(const void* k, const void* vt, int n, int cap) {
   if (!k || !vt) return fail(TADM_ERR_INVALID, "null keys or values");
@@ -1364,7 +1383,7 @@ tadm_status tadm_pages_append(tadm_model* m, const tadm_pages* p, int32_t layer,
                               const void* k_dev, const void* vt_dev, int32_t n, int32_t cap) {
   TRY(check_pages(p, layer));
   TRY(check_rows(rows));
-  if (n < 1) return fail(TADM_ERR_INVALID, "n=%d", n);
+  TRY(check_window_size(rows, n, 0));
   TRY(check_window_kv(k_dev, vt_dev, n, cap));
   if (!rows->len_dev && (long)rows->len + n > (long)rows->max_pages * PAGE)
     return fail(TADM_ERR_INVALID, "positions [%d, %ld) with %d pages a row", rows->len, (long)rows->len + n, rows->max_pages);
@@ -1375,15 +1394,8 @@ tadm_status tadm_pages_append(tadm_model* m, const tadm_pages* p, int32_t layer,
   return TADM_OK;
 }
 
-static tadm_status check_queries(const tadm_model* m, const tadm_page_rows* rows, int n) {
-  if (!m) return fail(TADM_ERR_INVALID, "null model");
-  if ((int64_t)rows->B * m->cfg.n_heads * n > INT32_MAX)
-    return fail(TADM_ERR_INVALID, "%d rows of %d queries: too many in one call", rows->B, n);
-  return TADM_OK;
-}
-
 size_t tadm_pages_attend_work(const tadm_model* m, const tadm_page_rows* rows, int32_t n) {
-  if (check_rows(rows) != TADM_OK || n < 1 || check_queries(m, rows, n) != TADM_OK) return 0;
+  if (check_rows(rows) != TADM_OK || !m || check_window_size(rows, n, m->cfg.n_heads) != TADM_OK) return 0;
   return page_attend_work(m->dt, rows->B, m->cfg.n_heads, m->cfg.n_kv_heads, m->cfg.head_dim, n, rows->len);
 }
 
@@ -1392,13 +1404,13 @@ tadm_status tadm_pages_attend(tadm_model* m, const tadm_pages* p, int32_t layer,
                               void* o_dev, float* lse_dev, void* work_dev, size_t work_bytes) {
   TRY(check_pages(p, layer));
   TRY(check_rows(rows));
-  if (n < 1) return fail(TADM_ERR_INVALID, "n=%d", n);
+  TRY(check_window_size(rows, n, 0));
   if (!q_dev || !o_dev) return fail(TADM_ERR_INVALID, "null queries or output");
   if (!aligned(q_dev, 16) || !aligned(o_dev, 16) || !aligned(lse_dev, 4))
     return fail(TADM_ERR_INVALID, "queries or output not aligned to 16 bytes");
   if (k_dev || vt_dev) TRY(check_window_kv(k_dev, vt_dev, n, cap));
-  TRY(check_queries(m, rows, n));
   TRY(check_page_model(m, p));
+  TRY(check_window_size(rows, n, m->cfg.n_heads));
   const size_t need = tadm_pages_attend_work(m, rows, n);
   if (need && (!work_dev || work_bytes < need || !aligned(work_dev, 16)))
     return fail(TADM_ERR_INVALID, "scratch of %zu bytes, %zu needed, aligned to 16", work_dev ? work_bytes : 0, need);
@@ -1478,6 +1490,7 @@ tadm_status tadm_pool_create(tadm_model* m, int32_t n_pages, tadm_pool** out) {
 tadm_status tadm_pool_destroy(tadm_pool* pool) {
   if (!pool) return fail(TADM_ERR_INVALID, "null pool");
   if (!pool->contexts.empty()) return fail(TADM_ERR_STATE, "%zu contexts still use the pool", pool->contexts.size());
+  OnDevice dev(pool->model->device);
   (void)hipDeviceSynchronize();
   (void)hipFree(pool->data);
   (void)hipFree(pool->scale);
@@ -1498,6 +1511,7 @@ tadm_status tadm_pool_pages(const tadm_pool* pool, tadm_pages* out) {
 tadm_status tadm_pool_compact(tadm_pool* pool) {
   if (!pool) return fail(TADM_ERR_INVALID, "null pool");
   tadm_model* m = pool->model;
+  TRY(check_no_capture(m, "moving pages"));
   OnDevice dev(m->device);
   HIPCHK(dev.err);
   try {

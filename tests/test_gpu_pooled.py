@@ -267,3 +267,50 @@ def test_pooled_refusals():
                 tadm.tadm_pool_create(w.m, n)
         tadm.tadm_context_destroy(plain)
         tadm.tadm_context_destroy(x)
+
+
+def test_captured_passes_follow_the_pages():
+    """A captured pass over a pooled context, replayed while its pages move, equals the eager one; appending
+    and moving pages are refused under capture and leave the context as it was."""
+    with World("bf16 128") as w:
+        first, ctx = w.context(), w.context()
+        w.append(first, w.tokens(130, 1))
+        w.append(ctx, w.tokens(100, 2))
+        B, n, z = w.B, 24, w.tokens(24, 3).to(dev())
+        want = w.step(ctx, z)
+        cache = tadm.tadm_cache_create(w.m, B, n)
+        logits = torch.empty(B, n, w.cfg["vocab"], device=dev())
+        nxt = torch.empty(B, n, dtype=torch.int32, device=dev())
+        more = w.tokens(70, 4).to(dev())
+
+        def run():
+            tadm.tadm_anchor_forward(w.m, ctx, z, B, n, 8, 8, cache)
+            tadm.tadm_denoise_step(w.m, ctx, z, B, n, 0, cache, tadm.step_args(8, 8, 3, 0, 4, 1.0), logits, nxt)
+
+        side, back = torch.cuda.Stream(), torch.cuda.current_stream()
+        side.wait_stream(back)
+        tadm.tadm_set_stream(w.m, side.cuda_stream)
+        with torch.cuda.stream(side):
+            run()
+        torch.cuda.synchronize()
+        free = tadm.tadm_pool_free_pages(w.pool)
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            for refused in (lambda: tadm.tadm_context_append(w.m, ctx, more, B, 70), lambda: tadm.tadm_pool_compact(w.pool)):
+                with pytest.raises(tadm.TadmError, match="captured"):
+                    refused()
+            run()
+        assert tadm.tadm_context_length(ctx) == 100 and tadm.tadm_pool_free_pages(w.pool) == free
+        for i in range(4):
+            if i == 2:  # the pages of ctx move
+                tadm.tadm_context_destroy(first)
+                with torch.cuda.stream(side):
+                    tadm.tadm_pool_compact(w.pool)
+            with torch.cuda.stream(side):
+                logits.zero_()
+                g.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(logits, want), i
+        tadm.tadm_set_stream(w.m, back.cuda_stream)
+        tadm.tadm_cache_destroy(cache)
+        tadm.tadm_context_destroy(ctx)

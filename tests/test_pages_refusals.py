@@ -136,3 +136,26 @@ def test_binding_refuses_wrong_tensors():
             tadm.page_set(d, s)
     with pytest.raises(ValueError):
         tadm.tadm_pages_copy(None, p, [1, 2], [3])
+
+
+@pytest.mark.parametrize("name", ["append", "attend"])
+@pytest.mark.parametrize("B, n", [(1, (1 << 26) + 1), (1, 2**31 - 64), (65535, 1025)])
+def test_windows_beyond_a_launch(name, B, n):
+    r = rows(B=B, max_pages=1 << 24, len=0)
+    assert call(name, r=r, n=n, cap=2**31 - 64) == INV
+    assert "2^26" in tadm.last_error()
+
+
+def test_binding_refuses_wrong_tables():
+    torch = pytest.importorskip("torch")
+    table, lens = torch.zeros(3, 4, dtype=torch.int32), torch.zeros(3, dtype=torch.int32)
+    r = tadm.page_rows(table, 100, lens, lens)
+    assert (r.B, r.max_pages, r.len) == (3, 4, 100)
+    for bad in (table.long(), table[:, ::2], table.T, table[0], table.float()):
+        with pytest.raises(ValueError):
+            tadm.page_rows(bad, 100)
+    for bad in (lens.long(), lens[:2], torch.zeros(6, dtype=torch.int32)[::2], lens[:, None]):
+        with pytest.raises(ValueError):
+            tadm.page_rows(table, 100, bad)
+        with pytest.raises(ValueError):
+            tadm.page_rows(table, 100, None, bad)
