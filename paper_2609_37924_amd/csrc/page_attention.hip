@@ -197,7 +197,9 @@ __device__ __forceinline__ f32x4 f32_codes(uint32_t c, float s) {
 }
 
 // Four waves on a strip of 16 columns, each taking every fourth tile; NB: head width in blocks of
-// 16, the last of which may be partial.
+// 16, the last of which may be partial.  Products and probabilities stay in float32.  float32 models are small
+// (at most 4 096 positions of a window), and what bounds them is a launch and one tile's latency: 5 rows of
+// 24 tokens over up to 333 positions, 4 heads x 16, 7.4 us, of which an empty launch takes 3.6.
 template <int NB>
 __global__ __launch_bounds__(256) void attend_f32_kernel(Args a) {
   constexpr int NW = 4;
@@ -406,6 +408,14 @@ __device__ __forceinline__ void window_tile(const Args& a, const Block& x, int w
 
 // Few columns: NW waves on the same 16 QS columns, each taking every NW-th tile straight from
 // memory into registers; the codes of the next tile are on their way while one is computed.
+//
+// Bound by the pages' bytes: no wave reads what another does, so LDS would only add a way, and
+// with a tile on its way per wave eight waves keep 128 KB a CU outstanding (128 elements a key).  16 tokens
+// over up to 8 192 positions, 32/16 heads x 128 (412 MB): 81 us, 5.1 TB/s, the rate of a copy of 1 GiB
+// on the same card (blocks of four waves took 101 where those of eight took 85).  1 token over 131 071
+// positions, 16/4 heads x 128 (134 MB): 35 with the join of its splits, 26 at the copy's rate.  1 token over
+// 200 positions: 7.7, of which an empty launch takes 3.6; the rest is loads that wait for one
+// another (lengths and table, scales, codes, the window) and the join of the waves.
 template <int DH, int QS, int NW>
 __global__ __launch_bounds__(64 * NW) void attend_narrow_kernel(Args a) {
   constexpr int NB = DH / 16;
@@ -516,6 +526,13 @@ __device__ __forceinline__ int swizzle(int row) {
 // exponentials, so that each SIMD has a wave for its matrix core and one for its vector unit.
 // A barrier of the whole block ends every such half step.  A step's V and the next one's K go to
 // LDS beside the matrix products.
+//
+// Bound by the half steps, the products' against the exponentials': 4 rows of 256 tokens over 16 384
+// positions, 32/16 heads x 128 (279 Gflop): 290 us, 960 TFLOP/s; at the 1 318 of a large library
+// product 212.  A half step of products takes 2 060 to 2 340 cycles for 1 024 of matrix instructions a
+// wave, one of exponentials 1 050 to 1 600, both stretched by the other group's instructions.
+// Both groups at the same step took 331 where turns took 307; of the present form, K placed beside the
+// exponentials takes 296 and a second tile ahead in registers 327 to 353.
 //
 // The codes of a tile are converted to bf16, scaled, on their way to LDS, once for all waves
 // (with codes in LDS, converted by every wave, the step took 8 % more), the values 0 behind the
