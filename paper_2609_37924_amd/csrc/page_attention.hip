@@ -569,7 +569,8 @@ __global__ __launch_bounds__(128 * CW, 2) void attend_wide_kernel(Args a) {
   const uint8_t* base = a.p.data + (size_t)x.h * 2 * PAGE * DH;
   char* const sb = smem + kw * GROUP;
   const int kr = gl / KC, vr = gl / 8;
-  const int k_src = key_of<false>(kr >> 4, kr >> 2 & 3, kr & 3) * DH + gl % KC * 8;
+  auto k_first = [&](int l) { return key_of<false>(l / KC >> 4, l / KC >> 2 & 3, l / KC & 3) * DH + l % KC * 8; };
+  const int k_src = k_first(gl);
   const int k_dst = kr * 2 * DH + (gl % KC ^ swizzle<2 * DH>(kr)) * 16;
   const int v_dst = 2 * BUF + vr * 128 + (gl % 8 ^ swizzle<128>(vr)) * 16;
   auto k_next = [&](int j) { return key_of<false>(KROWS * j >> 4, 0, 0) * DH; };
@@ -614,10 +615,13 @@ __global__ __launch_bounds__(128 * CW, 2) void attend_wide_kernel(Args a) {
   };
   // the lane's places in a buffer: K row fr, chunks 4 e + grp; V^T row fr, chunks (8 keys) 4 c + grp
   int kofs[DH / 32], vofs[2];
+  auto places = [&](int fr) {
 #pragma unroll
-  for (int e = 0; e < DH / 32; ++e) kofs[e] = fr * 2 * DH + ((4 * e + grp) ^ swizzle<2 * DH>(fr)) * 16;
+    for (int e = 0; e < DH / 32; ++e) kofs[e] = fr * 2 * DH + ((4 * e + grp) ^ swizzle<2 * DH>(fr)) * 16;
 #pragma unroll
-  for (int e = 0; e < 2; ++e) vofs[e] = 2 * BUF + fr * 128 + ((4 * e + grp) ^ swizzle<128>(fr)) * 16;
+    for (int e = 0; e < 2; ++e) vofs[e] = 2 * BUF + fr * 128 + ((4 * e + grp) ^ swizzle<128>(fr)) * 16;
+  };
+  places(fr);
   auto add_pv = [&](int st) {  // O += V^T P of step st
     const char* from = sb + (st & 1) * BUF;
 #pragma unroll
@@ -658,13 +662,11 @@ __global__ __launch_bounds__(128 * CW, 2) void attend_wide_kernel(Args a) {
       p_operand(s[u], p[u]);
     }
   };
-  const bf16* q[QS];
 #pragma unroll
   for (int u = 0; u < QS; ++u)
-    q[u] = static_cast<const bf16*>(a.q) + (x.head * ncol + min(col0 + 16 * u + fr, ncol - 1)) * DH;
+    qs[u] = load_query<DH, false>(
+        static_cast<const bf16*>(a.q) + (x.head * ncol + min(col0 + 16 * u + fr, ncol - 1)) * DH, grp);
   if (steps) {
-#pragma unroll
-    for (int u = 0; u < QS; ++u) qs[u] = load_query<DH, false>(q[u], grp);
     const int page0 = at_lane(tb.page, 0);
     load_k(Tile{page0});  // before the scales are there
     load_v(Tile{page0});
@@ -704,12 +706,55 @@ __global__ __launch_bounds__(128 * CW, 2) void attend_wide_kernel(Args a) {
       __syncthreads();  // the group is done with V of the step before
       soften();
     }
+  }
+  // The window's tiles: as steps behind those of the pages, the groups side by side, their elements through
+  // registers to the same places in LDS.  The first are on their way beside the last product of the pages.
+  const int w0 = max(x.t0, x.np), wsteps = x.t1 > w0 ? (x.t1 - w0 + 1) / 2 : 0;
+  const int mine = w0 + (kw ^ ((w0 - x.t0) & 1));
+  bf16x8 wk[PER], wv[PER];
+  auto load_window = [&](int t) {  // behind the last: the first one's, with no keys
+    const size_t w = (size_t)(t < x.t1 ? t - x.np : 0) * PAGE;
+    int l = gl;
+    asm volatile("" : "+v"(l));  // the addresses are made here, and take no registers in the loops
+    const bf16* k = static_cast<const bf16*>(a.k) + (x.head * a.cap + w) * DH + k_first(l);
+    const bf16* v = static_cast<const bf16*>(a.vt) + (x.head * DH + l / 8) * a.cap + w + l % 8 * 8;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) wk[j] = *reinterpret_cast<const bf16x8*>(k + k_next(j));
+#pragma unroll
+    for (int j = 0; j < PER; ++j) wv[j] = *reinterpret_cast<const bf16x8*>(v + (size_t)(VROWS * j) * a.cap);
+  };
+  if (wsteps) load_window(mine);
+  if (steps) {
     __syncthreads();
     add_pv(steps - 1);
     if (!kw) __syncthreads();
   }
-  for (int t = max(x.t0, x.np); t < x.t1; ++t)
-    if (((t - x.t0) & 1) == kw) window_tile<DH, QS>(a, x, t - x.np, q, o, m_run, l_run);
+  for (int i = 0; i < wsteps; ++i) {
+    int f = fr;
+    asm volatile("" : "+v"(f));  // as in load_window
+    places(f);
+    const int st = steps + i, t = mine + 2 * i;
+    keys = t < x.t1 ? min(PAGE, x.n - (t - x.np) * PAGE) : 0;
+    if (keys < PAGE)
+#pragma unroll
+      for (int j = 0; j < PER; ++j)
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (gl % 8 * 8 + e >= keys) wv[j][e] = (bf16)0.f;
+    char* to = sb + (st & 1) * BUF;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+      *reinterpret_cast<bf16x8*>(to + k_dst + KROWS * j * 2 * DH) = wk[j];
+      *reinterpret_cast<bf16x8*>(to + v_dst + VROWS * j * 128) = wv[j];
+    }
+    __syncthreads();  // also: the group is done with the step before the last, whose buffers come next
+    if (i + 1 < wsteps) load_window(t + 2);
+    if (keys > 0) {
+      score(st);
+      soften();
+      add_pv(st);
+    }
+  }
   // the second group joins the first, a strip at a time
   float* w = reinterpret_cast<float*>(smem) + cw * NV * 64 + lane;
 #pragma unroll
