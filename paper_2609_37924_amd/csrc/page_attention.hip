@@ -146,9 +146,9 @@ __device__ __forceinline__ float inverse(const Args& a, float sum) { return a.S 
 // l and O in [wave][value][lane] floats; wave w sums the head-width blocks w, w + NW, ...
 template <class T, int NB, int NW>
 __device__ __forceinline__ void join_waves(const Args& a, const Block& x, int col, float m_run, float l_run,
-                                           const f32x4 (&o)[NB], float* xs) {
+                                           const f32x4 (&o)[NB], float* xs, int wave) {
   constexpr int NV = 2 + 4 * NB;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, grp = lane >> 4;
+  const int lane = threadIdx.x & 63, grp = lane >> 4;
   float l = l_run + xor16(l_run);
   l += xor32(l);
   float* w = xs + wave * NV * 64 + lane;
@@ -266,7 +266,7 @@ __global__ __launch_bounds__(256) void attend_f32_kernel(Args a) {
       }
     }
   }
-  join_waves<float, NB, NW>(a, x, col, m_run, l_run, o, xs);
+  join_waves<float, NB, NW>(a, x, col, m_run, l_run, o, xs, wave);
 }
 
 // ---------------------------------------------------------------- bf16 models
@@ -508,7 +508,7 @@ __global__ __launch_bounds__(64 * NW) void attend_narrow_kernel(Args a) {
     if ((t - x.t0) % NW == wave) window_tile<DH, QS>(a, x, t - x.np, q, o, m_run, l_run);
 #pragma unroll
   for (int u = 0; u < QS; ++u)
-    join_waves<bf16, NB, NW>(a, x, x.ct * 16 * QS + 16 * u + fr, m_run[u], l_run[u], o[u], xs);
+    join_waves<bf16, NB, NW>(a, x, x.ct * 16 * QS + 16 * u + fr, m_run[u], l_run[u], o[u], xs, wave);
 }
 
 // Slot of chunk c (16 bytes) of a row of 128 or 256 bytes in LDS: c ^ swizzle(row).  With it, and lane
@@ -545,7 +545,7 @@ __global__ __launch_bounds__(128 * CW, 2) void attend_wide_kernel(Args a) {
   constexpr int PER = SIDE / 8 / GT;                               // chunks (8 codes) of a side that a lane moves per tile
   constexpr int KROWS = GT / KC, VROWS = GT / 8;                   // rows of K and V^T that a group moves at once
   static_assert(PER * 8 * GT == SIDE && CW == 4, "a tile splits over the lanes of a group in whole blocks of 16 keys");
-  static_assert(CW * NV * 64 * 4 <= 2 * GROUP, "the groups are joined in the space of the tiles");
+  static_assert(2 * CW * NV * 64 * 4 <= 2 * GROUP, "the groups are joined in the space of the tiles");
   __shared__ __attribute__((aligned(16))) char smem[2 * GROUP];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), grp = lane >> 4,
             fr = lane & 15, cw = wave % CW, kw = wave / CW, gl = cw * 64 + lane;
@@ -755,40 +755,11 @@ __global__ __launch_bounds__(128 * CW, 2) void attend_wide_kernel(Args a) {
       add_pv(st);
     }
   }
-  // the second group joins the first, a strip at a time
-  float* w = reinterpret_cast<float*>(smem) + cw * NV * 64 + lane;
+  __syncthreads();  // every wave is done with the tiles
+  float* xs = reinterpret_cast<float*>(smem) + cw * 2 * NV * 64;  // of the two waves of a strip
 #pragma unroll
-  for (int u = 0; u < QS; ++u) {
-    float l = l_run[u] + xor16(l_run[u]);
-    l_run[u] = l + xor32(l);
-    __syncthreads();  // every wave is done with the tiles, or with the previous strip
-    if (kw == 1) {
-      w[0] = m_run[u];
-      w[64] = l_run[u];
-#pragma unroll
-      for (int d = 0; d < NB; ++d)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) w[(2 + 4 * d + j) * 64] = o[u][d][j];
-    }
-    __syncthreads();
-    if (kw == 0) {
-      const float m = fmaxf(m_run[u], w[0]);
-      const float f0 = __builtin_amdgcn_exp2f(m_run[u] - m), f1 = __builtin_amdgcn_exp2f(w[0] - m);
-      const float l = l_run[u] * f0 + w[64] * f1;
-      const int col = col0 + 16 * u + fr;
-      if (col < ncol && col % a.r.max_n < x.n) {
-        const float inv = inverse(a, l);
-#pragma unroll
-        for (int d = 0; d < NB; ++d) {
-          float r[4];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) r[j] = o[u][d][j] * f0 + w[(2 + 4 * d + j) * 64] * f1;
-          put4<bf16>(a, x, col, 16 * d + 4 * grp, inv, r);
-        }
-        if (grp == 0) put_ml(a, x, col, m, l);
-      }
-    }
-  }
+  for (int u = 0; u < QS; ++u)
+    join_waves<bf16, NB, 2>(a, x, col0 + 16 * u + fr, m_run[u], l_run[u], o[u], xs, kw);
 }
 
 // Joins the splits of a column: GROUPS groups of 32 lanes, four values of the head width a lane, take every
