@@ -528,11 +528,15 @@ __device__ __forceinline__ int swizzle(int row) {
 // LDS beside the matrix products.
 //
 // Bound by the half steps, the products' against the exponentials': 4 rows of 256 tokens over 16 384
-// positions, 32/16 heads x 128 (279 Gflop): 290 us, 960 TFLOP/s; at the 1 318 of a large library
+// positions, 32/16 heads x 128 (279 Gflop): 286 us, 979 TFLOP/s; at the 1 318 of a large library
 // product 212.  A half step of products takes 2 060 to 2 340 cycles for 1 024 of matrix instructions a
 // wave, one of exponentials 1 050 to 1 600, both stretched by the other group's instructions.
-// Both groups at the same step took 331 where turns took 307; of the present form, K placed beside the
-// exponentials takes 296 and a second tile ahead in registers 327 to 353.
+// Both groups at the same step took 331 where turns took 307, K placed beside the exponentials 296 where beside
+// the products 290, a second tile ahead in registers 327 to 353.
+//
+// With 64 columns (QS = 1) a step takes 3 100 cycles, the moves to LDS alone 800 to 1 100: 16 rows x 64 tokens over
+// up to 1 024 positions, 16/4 heads x 128: 19.6 us.  Keys of a tile halved between waves of 32
+// columns (half the reads of LDS), a second tile ahead and K beside the exponentials: 20.2 to 21.9.
 //
 // The codes of a tile are converted to bf16, scaled, on their way to LDS, once for all waves
 // (with codes in LDS, converted by every wave, the step took 8 % more), the values 0 behind the
@@ -836,15 +840,17 @@ struct Plan {
 };
 
 // Measured on one MI355X, in us a call with everything around it:
-//  - Blocks of 128 columns, unless those of 64 are needed to give every CU one (2 rows x 256 tokens over 1 000
-//    positions, 32/16 heads x 128: 34 with 64 columns, 43 with 128; 4 rows: 66 and 44).
+//  - Blocks of 128 columns, unless those of 64 are needed to give every CU one (4 rows x 256 tokens over 2 000
+//    positions, 16/4 heads x 128: 32 with 64 columns, 46 with 128; 16 rows x 128 over 1 024: 38 and 30).
 //  - At most a block per CU in all: 16 tokens over 8 192 positions (256 blocks) take 81, and 95 in two splits;
 //    1 token over 131 071 31 in 64 splits of 4 blocks, 34 in 32, and 46 in 128.
 //  - Few columns: a split has two tiles of 128 or four of 64 elements a key, from 9 and 25 tiles on (1 token,
 //    16/4 heads x 128, over 8 000 positions: 49 in one split, 11.7 in 32; over 300, 9.0 in one and 10.6 in two;
 //    12 heads x 64 over 1 000 positions, 17 tiles: 8.0 in one, 9.3 in 16).
-//  - Many: a split has eight tiles, four steps of its two groups (64 tokens, 32/16 heads x 128, over 4 000
-//    positions: 53 in one split, 26 in 8; 12 heads x 64, 2 rows over 500: 10.5 in one, 12.7 in two).
+//  - Many: a split has four tiles, two steps of its two groups, from 13 tiles on (64 tokens, 16/4 heads x 128, over
+//    750 positions: 16.3 in one split, 14.7 in four, over 500, 13.4 and 13.9; 32/16 heads over 4 000: 51 in
+//    one, 25.6 in four, 22.5 in 8; 12 heads x 64 over 4 000: 35 in one, 13.8 in 16; 2 rows over 500: 9.7
+//    in one, 12.4 in four).
 Plan plan(DType dt, int B, int H, int Hkv, int dh, int L, int max_len) {
   const int ncol = H / Hkv * L;
   const int tiles = (max_len + PAGE - 1) / PAGE + (L + PAGE - 1) / PAGE;
@@ -853,7 +859,7 @@ Plan plan(DType dt, int B, int H, int Hkv, int dh, int L, int max_len) {
   long most = tiles > 8 ? tiles / 4 : 1;  // float32
   if (dt == BF16 && ncol > 32) {
     p.width = blocks(128) < 256 ? 64 : 128;
-    most = tiles / 8;
+    most = tiles > 12 ? tiles / 4 : 1;
   } else if (dt == BF16) {
     p.width = ncol > 16 ? 32 : 16;
     most = dh > 64 ? (tiles > 8 ? tiles / 2 : 1) : (tiles > 24 ? tiles / 4 : 1);
