@@ -314,6 +314,44 @@ def test_attention_of_many_tiles_a_wave(Hkv, dh, n, length):
         assert np.all(np.abs(lse[0, h].double().cpu().numpy() - ref_lse[0]) <= tl[0])
 
 
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("paged", [True, False])
+def test_windows_of_several_tiles_in_full_blocks(dh, paged):
+    """Enough columns for blocks of 128: windows of none to three tiles, NaN behind their ends, behind odd and even
+    numbers of pages, and alone."""
+    rng = np.random.default_rng(dh)
+    H = Hkv = 16
+    spans = [(0, 130), (1, 64), (64, 65), (65, 1), (128, 128), (150, 0), (70, 129), (300, 100)]
+    if not paged:
+        spans = [(0, new) for _, new in spans]
+    B, n, mp, cap = len(spans), 130, 5, cap_of(130)
+    pages = random_pages(rng, B * mp, 1, Hkv, dh)
+    table = rng.permutation(B * mp).reshape(B, mp)
+    q = torch.from_numpy(rng.normal(size=(B, H, n, dh))).to(torch.bfloat16)
+    k, vt = window(rng, B, Hkv, cap, dh, "bf16")
+    for b, (_, new) in enumerate(spans):
+        k[b, :, new:], vt[b, :, :, new:], q[b, :, new:] = float("nan"), float("nan"), float("nan")
+    data, scale, p = to_gpu(pages)
+    m = model("bf16", H, Hkv, dh)
+    try:
+        o, lse = run_attend(m, "bf16", p, 0, table, [a for a, _ in spans], [b for _, b in spans],
+                            mp * 64 if paged else 0, q, k, vt, cap)
+    finally:
+        tadm.tadm_model_destroy(m)
+    o, lse = o.double().cpu().numpy().reshape(B, n, H, dh), lse.double().cpu().numpy()
+    for b, (length, new) in enumerate(spans):
+        assert np.all(o[b, new:] == 7.0) and np.all(lse[b, :, new:] == 7.0), f"row {b}: padding was written"
+        for h in (0, Hkv - 1) if new else ():
+            K, V, _ = P.Pages(pages.codes[:, :, h:h + 1].copy(), pages.scales[:, :, h:h + 1].copy()).read(0, table[b], length)
+            K = np.concatenate([K, k[b, h:h + 1, :new].double().numpy()], axis=1)
+            V = np.concatenate([V, vt[b, h:h + 1, :, :new].double().numpy().transpose(0, 2, 1)], axis=1)
+            qh = q[b, h:h + 1, :new].double().numpy()
+            ref, ref_lse = P.attend(qh, K, V)
+            to, tl = bounds("bf16", qh, K, V)
+            assert np.all(np.abs(o[b, :new, h:h + 1] - ref) <= to), (b, h)
+            assert np.all(np.abs(lse[b, h, :new] - ref_lse[0]) <= tl[0]), (b, h)
+
+
 def test_overlapping_graphs_with_scratch_of_their_own():
     """Two captured calls replayed at once on two streams, each with its own scratch, equal the eager ones."""
     rng = np.random.default_rng(8)
