@@ -766,6 +766,7 @@ __global__ __launch_bounds__(128 * CW, 2) void attend_wide_kernel(Args a) {
     join_waves<bf16, NB, 2>(a, x, col0 + 16 * u + fr, m_run[u], l_run[u], o[u], xs, kw);
 }
 
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 // Joins the splits of a column: GROUPS groups of 32 lanes, four values of the head width a lane, take every
 // GROUPS-th split and are summed in order; a block has eight groups.
 template <class T, int GROUPS>
@@ -780,24 +781,34 @@ __global__ __launch_bounds__(256) void join_kernel(Args a) {
   const bool mine = id < cols && j < row_new(a.r, b);
   if (GROUPS == 8 && !mine) return;  // the whole block
   const float* ml = part_ml(a, col_id, 0);
+  const float* po = part_o(a, col_id, 0) + (4 * i < dh ? 4 * i : 0);
+  // the group's first splits are on their way while the maximum waits for its loads
+  constexpr int AHEAD = 4;
+  f32x4 v[AHEAD];
+  f32x2 w[AHEAD];
+#pragma unroll
+  for (int e = 0; e < AHEAD; ++e) {
+    const int s = min(g8 + GROUPS * e, a.S - 1);
+    v[e] = *reinterpret_cast<const f32x4*>(po + (size_t)s * dh);
+    w[e] = *reinterpret_cast<const f32x2*>(ml + 2 * s);
+  }
   float m = M_NONE;
-  if (mine)
-    for (int s = i; s < a.S; s += 32) m = fmaxf(m, ml[2 * s]);
+  for (int s = i; s < a.S; s += 32) m = fmaxf(m, ml[2 * s]);
   m = row16_max(m);
   m = fmaxf(m, xor16(m));
-  const float* po = part_o(a, col_id, 0) + 4 * i;
   float r[4] = {0.f, 0.f, 0.f, 0.f}, sum = 0.f;
-  if (mine)
-#pragma unroll 4
-    for (int s = g8; s < a.S; s += GROUPS) {
-      const float f = __builtin_amdgcn_exp2f(ml[2 * s] - m);
-      sum += ml[2 * s + 1] * f;
-      if (4 * i < dh) {
-        const f32x4 v = *reinterpret_cast<const f32x4*>(po + (size_t)s * dh);
+  auto add = [&](const f32x4& v, const f32x2& w) {
+    const float f = __builtin_amdgcn_exp2f(w[0] - m);
+    sum += w[1] * f;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) r[e] += v[e] * f;
-      }
-    }
+    for (int e = 0; e < 4; ++e) r[e] += v[e] * f;
+  };
+#pragma unroll
+  for (int e = 0; e < AHEAD; ++e)
+    if (g8 + GROUPS * e < a.S) add(v[e], w[e]);
+#pragma unroll 4
+  for (int s = g8 + GROUPS * AHEAD; s < a.S; s += GROUPS)
+    add(*reinterpret_cast<const f32x4*>(po + (size_t)s * dh), *reinterpret_cast<const f32x2*>(ml + 2 * s));
   if constexpr (GROUPS > 1) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) xs[g8][4 * i + e] = r[e];
