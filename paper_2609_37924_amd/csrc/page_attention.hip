@@ -341,6 +341,8 @@ __device__ __forceinline__ float at_lane(float v, int lane) {
   return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane));
 }
 
+// Probabilities are rounded to bf16 here, for the bf16 products (at most 2^-8 of each, like the rounding of the
+// result; the sum l has them unrounded): float32 products are eight times slower.
 // Probabilities of a tile as the operand of O^T = V^T P^T: k index 8 grp + j of product c is the key of
 // score row 4 grp + j % 4 of block 2 c + j / 4.
 __device__ __forceinline__ void p_operand(const f32x4 (&s)[4], bf16x8 (&p)[2]) {
@@ -413,7 +415,7 @@ __device__ __forceinline__ void window_tile(const Args& a, const Block& x, int w
 // with a tile on its way per wave eight waves keep 128 KB a CU outstanding (128 elements a key).  16 tokens
 // over up to 8 192 positions, 32/16 heads x 128 (412 MB): 81 us, 5.1 TB/s, the rate of a copy of 1 GiB
 // on the same card (blocks of four waves took 101 where those of eight took 85).  1 token over 131 071
-// positions, 16/4 heads x 128 (134 MB): 35 with the join of its splits, 26 at the copy's rate.  1 token over
+// positions, 16/4 heads x 128 (134 MB): 32 with the join of its splits, 26 at the copy's rate.  1 token over
 // 200 positions: 7.7, of which an empty launch takes 3.6; the rest is loads that wait for one
 // another (lengths and table, scales, codes, the window) and the join of the waves.
 template <int DH, int QS, int NW>
@@ -831,13 +833,14 @@ __global__ __launch_bounds__(256) void join_kernel(Args a) {
   if (4 * i < dh) store4(out + 4 * i, r[0] * inv, r[1] * inv, r[2] * inv, r[3] * inv);
   if (i == 0 && a.lse) a.lse[col_id] = sum == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * LN2;
 }
-// Eight groups a column for many splits or few columns, where the loads of one group in a row are what takes
-// time (16 columns of 8 splits: 19.4 us with one group, 16.5 with eight, the attention included); else one,
-// which needs an eighth of the blocks (16 384 columns of 2 splits: 59 us with eight, 40 with one).
+// Eight groups a column from 9 splits on, where the loads of one group in a row are what takes time (96 columns
+// of 16 splits: 15.3 us with one group, 14.6 with eight, the attention included); else one, which
+// needs an eighth of the blocks (2 048 columns of 8 splits: 18.5 with one, 20.8 with eight; 16 columns of 8:
+// 10.0 and 9.9).  Bound by its launch and two loads behind one another.
 template <class T>
 void start_join(const Args& a, hipStream_t s) {
   const size_t cols = (size_t)a.r.B * a.p.Hkv * a.G * a.r.max_n;
-  if (a.S > 8 || cols <= 2048)
+  if (a.S > 8)
     hipLaunchKernelGGL((join_kernel<T, 8>), dim3((unsigned)cols), dim3(256), 0, s, a);
   else
     hipLaunchKernelGGL((join_kernel<T, 1>), dim3((unsigned)((cols + 7) / 8)), dim3(256), 0, s, a);
@@ -854,12 +857,13 @@ struct Plan {
 //  - Blocks of 128 columns, unless those of 64 are needed to give every CU one (4 rows x 256 tokens over 2 000
 //    positions, 16/4 heads x 128: 32 with 64 columns, 46 with 128; 16 rows x 128 over 1 024: 38 and 30).
 //  - At most a block per CU in all: 16 tokens over 8 192 positions (256 blocks) take 81, and 95 in two splits;
-//    1 token over 131 071 31 in 64 splits of 4 blocks, 34 in 32, and 46 in 128.
+//    1 token over 131 000 29 in 64 splits of 4 blocks, 33 in 32, and 34 in 128.
 //  - Few columns: a split has two tiles of 128 or four of 64 elements a key, from 9 and 25 tiles on (1 token,
-//    16/4 heads x 128, over 8 000 positions: 49 in one split, 11.7 in 32; over 300, 9.0 in one and 10.6 in two;
+//    16/4 heads x 128, over 8 000 positions: 12.7 in 16 splits, 10.7 in 32 and 64; over 1 000, 13.7 in one and
+//    10.2 in 8; over 300, 8.5 in one and 10.2 in two;
 //    12 heads x 64 over 1 000 positions, 17 tiles: 8.0 in one, 9.3 in 16).
 //  - Many: a split has four tiles, two steps of its two groups, from 13 tiles on (64 tokens, 16/4 heads x 128, over
-//    750 positions: 16.3 in one split, 14.7 in four, over 500, 13.4 and 13.9; 32/16 heads over 4 000: 51 in
+//    750 positions: 16.3 in one split, 14.7 in four; over 500, 13.4 and 13.9; 32/16 heads over 4 000: 51 in
 //    one, 25.6 in four, 22.5 in 8; 12 heads x 64 over 4 000: 35 in one, 13.8 in 16; 2 rows over 500: 9.7
 //    in one, 12.4 in four).
 Plan plan(DType dt, int B, int H, int Hkv, int dh, int L, int max_len) {
