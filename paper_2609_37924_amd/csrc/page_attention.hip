@@ -342,7 +342,7 @@ __device__ __forceinline__ float at_lane(float v, int lane) {
 }
 
 // Probabilities are rounded to bf16 here, for the bf16 products (at most 2^-8 of each, like the rounding of the
-// result; the sum l has them unrounded): float32 products are eight times slower.
+// result; the sum l has them unrounded): float32 products are sixteen times slower.
 // Probabilities of a tile as the operand of O^T = V^T P^T: k index 8 grp + j of product c is the key of
 // score row 4 grp + j % 4 of block 2 c + j / 4.
 __device__ __forceinline__ void p_operand(const f32x4 (&s)[4], bf16x8 (&p)[2]) {
