@@ -36,6 +36,9 @@ static tadm_status fail(tadm_status st, const char* fmt, ...) {
   std::vsnprintf(buf, sizeof buf, fmt, ap);
   va_end(ap);
   g_err = buf;
+  // the runtime keeps a failed call's error until it is asked for it: unasked, the check behind the next launch,
+  // which may be sound, would find it
+  if (st == TADM_ERR_OOM || st == TADM_ERR_DEVICE) (void)hipGetLastError();
   return st;
 }
 
