@@ -268,8 +268,9 @@ tadm_status tadm_pool_resize(tadm_pool* pool, int32_t n_pages);
  * returns TADM_ERR_OOM, without side effects, when the pool has too few.  reset and
  * destroy give them back.  tadm_context_read returns the pages' values.  Passes over the
  * context may be captured and find its pages where they are at each replay, at the length
- * of the capture; tadm_context_append may not (TADM_ERR_STATE), since a replay would write
- * to pages that others may hold by then. */
+ * of the capture (positions whose pages it gave back since then take no part); creating it,
+ * tadm_context_append, and the truncate or reset that gives back pages may not
+ * (TADM_ERR_STATE), since a replay would use pages that others may hold by then. */
 tadm_status tadm_context_create_pooled(tadm_model* m, tadm_pool* pool, int32_t B, int32_t max_ctx,
                                        tadm_context** out);
 /* A new context of B rows with the length and capacity of `src`, row b holding what row rows[b] (host
@@ -280,7 +281,8 @@ tadm_status tadm_context_fork(const tadm_context* src, const int32_t* rows, int3
 /* Drops the positions [len, tadm_context_length) of any context; a pooled one gives back the
  * pages that hold none of the others. */
 tadm_status tadm_context_truncate(tadm_context* ctx, int32_t len);
-/* The rows of a pooled context for the operators above (valid until it is destroyed; len as of now). */
+/* The rows of a pooled context for the operators above (valid until it is destroyed; len as of now).
+ * Behind the context's pages the table has absent ones. */
 tadm_status tadm_context_rows(const tadm_context* ctx, tadm_page_rows* out);
 
 /* ------------------------------------------------------------ the step ---- */

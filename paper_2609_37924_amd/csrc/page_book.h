@@ -15,6 +15,13 @@ struct PageTable {
   PageTable(int rows, int per_row) : rows(rows), per_row(per_row), id((size_t)rows * per_row, -1) {}
   int32_t& at(int b, int i) { return id[(size_t)b * per_row + i]; }
   int32_t at(int b, int i) const { return id[(size_t)b * per_row + i]; }
+  // whether a row has a page in [from, per_row)
+  bool any(int from) const {
+    for (int b = 0; b < rows; ++b)
+      for (int i = from; i < per_row; ++i)
+        if (at(b, i) >= 0) return true;
+    return false;
+  }
 };
 
 // Page dst[i] takes what page src[i] has; entry at[i] of a table becomes to[i].

@@ -46,6 +46,8 @@ hipError_t pages_copy(void* data, float* scale, size_t page_bytes, size_t page_s
 
 // table[at[i]] = id[i] (host arrays, copied into the launches).
 hipError_t table_set(int32_t* table, const int32_t* at, const int32_t* id, int n, hipStream_t s);
+// The entries [from, per_row) of every row name no page (-1).
+hipError_t table_clear(int32_t* table, int rows, int per_row, int from, hipStream_t s);
 
 // Attention of the window's queries q [B, H, L, dh] (L = r.max_n) over the committed positions
 // and, with k, the window's own keys: o [B, L, H dh], lse (nullable) [B, H, L].  Rows at and

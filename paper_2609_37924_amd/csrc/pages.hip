@@ -290,6 +290,11 @@ __global__ __launch_bounds__(512) void table_set_kernel(int32_t* table, CopyPair
   if (i < n) table[pairs.src[i]] = pairs.dst[i];
 }
 
+__global__ __launch_bounds__(256) void table_clear_kernel(int32_t* table, int rows, int per_row, int from) {
+  const int i = blockIdx.x * 256 + threadIdx.x, w = per_row - from;
+  if (i < rows * w) table[(size_t)(i / w) * per_row + from + i % w] = -1;
+}
+
 // pairs [i, i + COPY_PAIRS) of two lists of n, unused places 0
 CopyPairs some_pairs(const int32_t* a, const int32_t* b, int i, int n, int* m) {
   CopyPairs pairs{};
@@ -311,6 +316,13 @@ hipError_t table_set(int32_t* table, const int32_t* at, const int32_t* id, int n
     if (e != hipSuccess) return e;
   }
   return hipSuccess;
+}
+
+hipError_t table_clear(int32_t* table, int rows, int per_row, int from, hipStream_t s) {
+  if (from >= per_row) return hipSuccess;
+  const unsigned blocks = ((unsigned)rows * (per_row - from) + 255) / 256;
+  hipLaunchKernelGGL(table_clear_kernel, dim3(blocks), dim3(256), 0, s, table, rows, per_row, from);
+  return hipGetLastError();
 }
 
 hipError_t pages_append(DType dt, const PageLayer& p, const PageRows& r, const void* k, const void* vt, int cap,

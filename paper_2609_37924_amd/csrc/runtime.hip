@@ -1206,19 +1206,47 @@ int32_t tadm_cache_refresh_step(const tadm_cache* c) { return c ? c->refresh_i :
 // ---------------------------------------------------------------- context ---
 }  // extern "C"
 
-// Keeps the positions [0, len): a pooled context gives back the pages that hold no others.
-static void context_drop(tadm_context* x, int len) {
-  x->len = len;
-  if (x->pool) x->pool->book.drop(x->table, (len + PAGE - 1) / PAGE);
-}
+// The model's device for the duration of a call.
+namespace {
+struct OnDevice {
+  int prev = -1;
+  hipError_t err;
+  explicit OnDevice(int device) {
+    err = hipGetDevice(&prev);
+    if (err == hipSuccess && prev != device)
+      err = hipSetDevice(device);
+    else
+      prev = -1;
+  }
+  ~OnDevice() {
+    if (prev >= 0) (void)hipSetDevice(prev);
+  }
+};
+}  // namespace
 
-// Pages are handed out by the host as calls are enqueued; a replay would hand out those of the capture
-// again, whoever holds them by then.
+// Pages are handed out and taken back by the host as calls are enqueued; a replay would do what the capture did
+// again, whoever holds the pages by then.
 static tadm_status check_no_capture(const tadm_model* m, const char* what) {
   if (!m->stream) return TADM_OK;  // the null stream is never captured
   hipStreamCaptureStatus st;
   HIPCHK(hipStreamIsCapturing(m->stream, &st));
   return st == hipStreamCaptureStatusNone ? TADM_OK : fail(TADM_ERR_STATE, "%s cannot be captured", what);
+}
+
+// Keeps the positions [0, len): a pooled context gives back the pages that hold no others, and its table on the
+// device no longer names them, since others may hold them next.
+static tadm_status context_drop(tadm_context* x, int len) {
+  const int keep = (len + PAGE - 1) / PAGE;
+  if (x->pool && x->table.any(keep)) {
+    tadm_model* m = x->model;
+    TRY(check_no_capture(m, "giving back pages"));
+    OnDevice dev(m->device);
+    HIPCHK(dev.err);
+    HIPCHK(table_clear(x->table_dev, x->table.rows, x->table.per_row, keep, m->stream));
+    x->pool->book.drop(x->table, keep);
+  }
+  x->len = len;
+  return TADM_OK;
 }
 
 // Gives every row of a pooled context pages of its own for the positions [len, len + n).
@@ -1273,15 +1301,13 @@ int32_t tadm_context_length(const tadm_context* ctx) { return ctx ? ctx->len : 0
 
 tadm_status tadm_context_reset(tadm_context* ctx) {
   if (!ctx) return fail(TADM_ERR_INVALID, "null context");
-  context_drop(ctx, 0);
-  return TADM_OK;
+  return context_drop(ctx, 0);
 }
 
 tadm_status tadm_context_truncate(tadm_context* ctx, int32_t len) {
   if (!ctx) return fail(TADM_ERR_INVALID, "null context");
   if (len < 0 || len > ctx->len) return fail(TADM_ERR_INVALID, "length %d of a context of %d positions", len, ctx->len);
-  context_drop(ctx, len);
-  return TADM_OK;
+  return context_drop(ctx, len);
 }
 
 tadm_status tadm_context_destroy(tadm_context* ctx) {
@@ -1290,7 +1316,7 @@ tadm_status tadm_context_destroy(tadm_context* ctx) {
   for (void* p : ctx->k) (void)hipFree(p);
   for (void* p : ctx->vt) (void)hipFree(p);
   if (ctx->pool) {
-    context_drop(ctx, 0);
+    ctx->pool->book.drop(ctx->table, 0);
     auto& all = ctx->pool->contexts;
     all.erase(std::remove(all.begin(), all.end(), ctx), all.end());
   }
@@ -1303,25 +1329,7 @@ tadm_status tadm_context_destroy(tadm_context* ctx) {
 // ----------------------------------------------------- paged 8-bit K/V ---
 }  // extern "C"
 
-// The model's device for the duration of a call.
-namespace {
-struct OnDevice {
-  int prev = -1;
-  hipError_t err;
-  explicit OnDevice(int device) {
-    err = hipGetDevice(&prev);
-    if (err == hipSuccess && prev != device)
-      err = hipSetDevice(device);
-    else
-      prev = -1;
-  }
-  ~OnDevice() {
-    if (prev >= 0) (void)hipSetDevice(prev);
-  }
-};
-
-bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
-}  // namespace
+static bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
 
 // The arguments are checked before the model, so that a call without one names what is wrong with them.
 static tadm_status check_pages(const tadm_pages* p, int layer) {
@@ -1581,7 +1589,7 @@ tadm_status tadm_pool_resize(tadm_pool* pool, int32_t n_pages) {
 
 }  // extern "C"
 
-// A pooled context without pages; its scratch covers every window that its positions allow.
+// A pooled context without pages, its table on the device naming none; its scratch covers every window that its positions allow.
 static tadm_status pooled_create(tadm_pool* pool, int B, int cap, tadm_context** out) {
   tadm_model* m = pool->model;
   OnDevice dev(m->device);
@@ -1604,6 +1612,7 @@ static tadm_status pooled_create(tadm_pool* pool, int B, int cap, tadm_context**
       x->work_bytes = std::max(x->work_bytes, page_attend_work(m->dt, B, m->cfg.n_heads, m->cfg.n_kv_heads,
                                                                m->cfg.head_dim, n, len));
   hipError_t e = hipMalloc((void**)&x->table_dev, x->table.id.size() * 4);
+  if (e == hipSuccess) e = table_clear(x->table_dev, B, x->table.per_row, 0, m->stream);
   if (e == hipSuccess) e = hipMalloc(&x->work, std::max<size_t>(x->work_bytes, 256));
   if (e != hipSuccess) {
     tadm_context_destroy(x);
@@ -1622,6 +1631,7 @@ tadm_status tadm_context_create_pooled(tadm_model* m, tadm_pool* pool, int32_t B
   if (pool->model != m) return fail(TADM_ERR_STATE, "pool belongs to another model");
   if (B < 1 || B > m->cfg.max_batch || max_ctx < 1 || max_ctx > m->cfg.max_seq)
     return fail(TADM_ERR_INVALID, "context shape B=%d max_ctx=%d outside the model limits", B, max_ctx);
+  TRY(check_no_capture(m, "creating a pooled context"));
   return pooled_create(pool, B, round64(max_ctx), out);
 }
 

@@ -1,6 +1,9 @@
 """What a page pool and its contexts must not do to one another, and the calls that they refuse."""
+import numpy as np
 import pytest
 import torch
+
+from oracle import pages as P
 
 pytestmark = pytest.mark.gpu
 
@@ -9,7 +12,19 @@ tadm = pytest.importorskip("paper_2609_37924_amd")
 if not torch.cuda.is_available():
     pytest.skip("no GPU", allow_module_level=True)
 
+from test_gpu_pages import bounds  # noqa: E402
 from test_gpu_pooled import World  # noqa: E402
+from helpers import dev  # noqa: E402
+
+
+def pages_seen(w, ctx, layer=0):
+    """Which places of each row's table name a page, as an operator over all of them finds them ([B, max_pages])."""
+    r, hk, dh = tadm.tadm_context_rows(ctx), w.cfg["n_kv_heads"], w.cfg["head_dim"]
+    r.len = r.max_pages * 64
+    k = torch.full((r.B, hk, r.len, dh), 7.0, dtype=w.dt, device=dev())
+    vt = torch.full((r.B, hk, dh, r.len), 7.0, dtype=w.dt, device=dev())
+    tadm.tadm_pages_read(w.m, tadm.tadm_pool_pages(w.pool), layer, r, k, vt, r.len)
+    return (k.abs().amax((1, 3)) > 0).view(r.B, -1, 64).any(2).tolist()  # an absent page reads as zeros
 
 
 def test_calls_after_an_allocation_that_failed():
@@ -29,3 +44,86 @@ def test_calls_after_an_allocation_that_failed():
         assert all((x[:, :, :64] == y).all() for u, v in zip(before, w.read(ctx)) for x, y in zip(u, v))
         tadm.tadm_context_destroy(ctx)
         tadm.tadm_context_destroy(plain)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16 128"])
+def test_a_table_names_the_pages_of_its_context_alone(kind):
+    """On the device too, places that never had a page or whose page was given back name none, whoever has it now."""
+    with World(kind, pages=24) as w:
+        filled = w.context()
+        w.append(filled, w.tokens(300, 1))  # 10 pages, none of them empty when it lets go of them
+        tadm.tadm_context_destroy(filled)
+        ctx, other = w.context(), w.context(B=1)
+        holds = lambda n: [[i < n for i in range(7)]] * 2  # noqa: E731
+        assert pages_seen(w, ctx) == holds(0)
+        w.append(ctx, w.tokens(330, 2))
+        assert pages_seen(w, ctx) == holds(6)
+        kid = tadm.tadm_context_fork(ctx, [1, 0])
+        assert pages_seen(w, kid) == holds(6)
+        for keep, n in ((330, 6), (321, 6), (320, 5), (193, 4), (128, 2), (100, 2)):
+            tadm.tadm_context_truncate(ctx, keep)
+            assert pages_seen(w, ctx) == holds(n), keep
+        tadm.tadm_context_destroy(kid)
+        w.append(other, w.tokens(400, 3, 1))  # takes pages that ctx had
+        assert pages_seen(w, ctx) == holds(2)
+        w.append(ctx, w.tokens(100, 4))
+        assert pages_seen(w, ctx) == holds(4)
+        tadm.tadm_context_reset(ctx)
+        assert pages_seen(w, ctx) == holds(0)
+        for x in (ctx, other):
+            tadm.tadm_context_destroy(x)
+        assert tadm.tadm_pool_free_pages(w.pool) == 24
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16 128"])
+def test_a_captured_call_after_a_rollback(kind):
+    """Attention over a context's rows, captured at 130 positions and replayed after the context fell back to 64
+    and another took the pages it gave back: equals the oracle over the 64 positions, replay after replay; what
+    gives back or takes pages is refused under capture and changes nothing."""
+    with World(kind) as w:
+        ctx, other = w.context(), w.context()
+        w.append(ctx, w.tokens(130, 1))
+        H, hk, dh, n = w.cfg["n_heads"], w.cfg["n_kv_heads"], w.cfg["head_dim"], 5
+        q = torch.randn(w.B, H, n, dh, device=dev()).to(w.dt)
+        o = torch.zeros(w.B, n, H * dh, dtype=w.dt, device=dev())
+        p, r = tadm.tadm_pool_pages(w.pool), tadm.tadm_context_rows(ctx)
+        work = torch.empty(max(16, tadm.tadm_pages_attend_work(w.m, r, n)), dtype=torch.uint8, device=dev())
+        call = lambda: tadm.tadm_pages_attend(w.m, p, 1, r, q, n, None, None, 0, o, None, work)  # noqa: E731
+
+        def check(length):
+            k, v = w.read(ctx)[1]
+            for b in range(w.B):
+                qb = q[b].double().cpu().numpy()
+                ref, _ = P.attend(qb, k[b][:, :length], v[b][:, :length])
+                to, _ = bounds("f32" if w.dt == torch.float32 else "bf16", qb, k[b][:, :length], v[b][:, :length])
+                assert np.all(np.abs(o[b].double().cpu().numpy().reshape(n, H, dh) - ref) <= to)
+
+        call()
+        check(130)
+        side, back = torch.cuda.Stream(), torch.cuda.current_stream()
+        free = tadm.tadm_pool_free_pages(w.pool)
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            tadm.tadm_set_stream(w.m, side.cuda_stream)
+            for refused in (lambda: tadm.tadm_context_truncate(ctx, 128), lambda: tadm.tadm_context_reset(ctx),
+                            lambda: w.context()):
+                with pytest.raises(tadm.TadmError, match="captured") as e:
+                    refused()
+                assert e.value.status == tadm.TADM_ERR_STATE
+            tadm.tadm_context_truncate(ctx, 130)  # gives nothing back
+            tadm.tadm_context_reset(other)
+            call()
+        tadm.tadm_set_stream(w.m, back.cuda_stream)
+        assert tadm.tadm_context_length(ctx) == 130 and tadm.tadm_pool_free_pages(w.pool) == free
+        for length in (130, 128, 64, 64):
+            tadm.tadm_context_truncate(ctx, length)
+            tadm.tadm_context_reset(other)
+            w.append(other, w.tokens(250, length))
+            o.zero_()
+            torch.cuda.synchronize()
+            g.replay()
+            torch.cuda.synchronize()
+            check(length)
+        for x in (ctx, other):
+            tadm.tadm_context_destroy(x)
