@@ -276,7 +276,7 @@ tadm_status tadm_context_create_pooled(tadm_model* m, tadm_pool* pool, int32_t B
 /* A new context of B rows with the length and capacity of `src`, row b holding what row rows[b] (host
  * array; a row may be taken several times) of src holds.  The pages are shared until one
  * of their holders appends to a page that others hold too, which first copies that page.
- * src must be a pooled context (TADM_ERR_STATE otherwise). */
+ * src must be a pooled context and the call is not captured (TADM_ERR_STATE otherwise). */
 tadm_status tadm_context_fork(const tadm_context* src, const int32_t* rows, int32_t B, tadm_context** out);
 /* Drops the positions [len, tadm_context_length) of any context; a pooled one gives back the
  * pages that hold none of the others. */

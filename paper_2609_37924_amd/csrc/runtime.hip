@@ -1640,6 +1640,7 @@ tadm_status tadm_context_fork(const tadm_context* src, const int32_t* rows, int3
   *out = nullptr;
   if (!src->pool) return fail(TADM_ERR_STATE, "only pooled contexts can be forked");
   tadm_model* m = src->model;
+  TRY(check_no_capture(m, "forking a context"));
   if (B < 1 || B > m->cfg.max_batch) return fail(TADM_ERR_INVALID, "B=%d outside [1, %d]", B, m->cfg.max_batch);
   for (int b = 0; b < B; ++b)
     if (rows[b] < 0 || rows[b] >= src->B) return fail(TADM_ERR_INVALID, "row %d of a context of %d rows", rows[b], src->B);

@@ -127,3 +127,41 @@ def test_a_captured_call_after_a_rollback(kind):
             check(length)
         for x in (ctx, other):
             tadm.tadm_context_destroy(x)
+
+
+def test_forks_under_capture_are_refused():
+    """A fork within a capture is refused, leaves no trace in the pool and does not disturb the capture; forked
+    before it, the new context runs the captured pass like the old one, while the old one goes on."""
+    with World("bf16 128") as w:
+        root = w.context()
+        w.append(root, w.tokens(100, 1))
+        kid = tadm.tadm_context_fork(root, [0, 1])
+        B, n, z = w.B, 16, w.tokens(16, 2).to(dev())
+        want, free = w.step(root, z), tadm.tadm_pool_free_pages(w.pool)
+        cache = tadm.tadm_cache_create(w.m, B, n)
+        logits = torch.empty(B, n, w.cfg["vocab"], device=dev())
+        nxt = torch.empty(B, n, dtype=torch.int32, device=dev())
+        side, back = torch.cuda.Stream(), torch.cuda.current_stream()
+        tadm.tadm_set_stream(w.m, side.cuda_stream)
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            for rows in ([0, 1], [1]):
+                with pytest.raises(tadm.TadmError, match="captured") as e:
+                    tadm.tadm_context_fork(root, rows)
+                assert e.value.status == tadm.TADM_ERR_STATE
+            tadm.tadm_anchor_forward(w.m, kid, z, B, n, 8, 8, cache)
+            tadm.tadm_denoise_step(w.m, kid, z, B, n, 0, cache, tadm.step_args(8, 8, 3, 0, 4, 1.0), logits, nxt)
+        tadm.tadm_set_stream(w.m, back.cuda_stream)
+        assert tadm.tadm_pool_free_pages(w.pool) == free
+        for i in range(4):
+            w.append(root, w.tokens(10, 20 + i))  # copies the page that it shares with the fork, then goes on alone
+            logits.zero_()
+            torch.cuda.synchronize()
+            g.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(logits, want), i
+        tadm.tadm_cache_destroy(cache)
+        for x in (root, kid):
+            tadm.tadm_context_destroy(x)
+        assert tadm.tadm_pool_free_pages(w.pool) == 40
