@@ -211,7 +211,9 @@ typedef struct {
  * the larger of the present one and 2^e, and their codes are rounded again if it grew.
  * code(x) = x / scale rounded to nearest even; infinities and NaN become the NaN code.
  * Codes of other positions stay as they are, and so do the rows' lengths (the caller
- * advances them).  No two rows may write the same page. */
+ * advances them).  No page may be written twice in a call, by two rows or by one.  The rows of
+ * a pooled context (tadm_context_rows) are not for appending (TADM_ERR_STATE): its pages may be
+ * shared, and tadm_context_append parts them. */
 tadm_status tadm_pages_append(tadm_model* m, const tadm_pages* p, int32_t layer, const tadm_page_rows* rows,
                               const void* k_dev, const void* vt_dev, int32_t n, int32_t cap);
 /* Attention of a window over the rows' pages of one layer: for every query q_dev

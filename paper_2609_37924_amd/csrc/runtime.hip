@@ -11,6 +11,7 @@
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
+#include <functional>
 #include <mutex>
 #include <string>
 #include <vector>
@@ -300,6 +301,7 @@ struct tadm_model {
   // profiling
   int32_t prof_mask = 0;  // bit s: record stage s
   std::vector<ProfRec> recs;
+  std::vector<tadm_pool*> page_pools;
   std::vector<hipEvent_t> pool;
   std::vector<OpenStage> open;  // stages begun and not yet ended
 
@@ -1378,6 +1380,17 @@ static tadm_status check_window_kv(const void* k, const void* vt, int n, int cap
   return TADM_OK;
 }
 
+// The rows of a pooled context are read-only: its last page may be others' too, and what is written behind its
+// length raises the scales that its committed positions have.  Only tadm_context_append takes pages for it.
+static tadm_status check_own_table(const tadm_model* m, const tadm_page_rows* r) {
+  for (const tadm_pool* p : m->page_pools)
+    for (const tadm_context* x : p->contexts)
+      if (!std::less<const int32_t*>()(r->table_dev, x->table_dev) &&
+          std::less<const int32_t*>()(r->table_dev, x->table_dev + x->table.id.size()))
+        return fail(TADM_ERR_STATE, "appending to the rows of a pooled context (tadm_context_append does)");
+  return TADM_OK;
+}
+
 static PageLayer page_layer(const tadm_pages* p, int layer) {
   const size_t bytes = (size_t)p->n_kv_heads * 2 * PAGE * p->head_dim;
   return PageLayer{static_cast<uint8_t*>(p->data) + layer * bytes, p->scale + (size_t)layer * 2 * p->n_kv_heads,
@@ -1399,6 +1412,7 @@ tadm_status tadm_pages_append(tadm_model* m, const tadm_pages* p, int32_t layer,
   if (!rows->len_dev && (long)rows->len + n > (long)rows->max_pages * PAGE)
     return fail(TADM_ERR_INVALID, "positions [%d, %ld) with %d pages a row", rows->len, (long)rows->len + n, rows->max_pages);
   TRY(check_page_model(m, p));
+  TRY(check_own_table(m, rows));
   OnDevice dev(m->device);
   HIPCHK(dev.err);
   HIPCHK(pages_append(m->dt, page_layer(p, layer), page_rows(rows, n), k_dev, vt_dev, cap, m->stream));
@@ -1480,6 +1494,7 @@ tadm_status tadm_pool_create(tadm_model* m, int32_t n_pages, tadm_pool** out) {
   HIPCHK(dev.err);
   tadm_pool* p = nullptr;
   try {
+    m->page_pools.reserve(m->page_pools.size() + 1);
     p = new tadm_pool{m, PageBook(n_pages)};
   } catch (const std::exception&) {
     return fail(TADM_ERR_OOM, "host memory");
@@ -1494,6 +1509,7 @@ tadm_status tadm_pool_create(tadm_model* m, int32_t n_pages, tadm_pool** out) {
     return fail(e == hipErrorOutOfMemory ? TADM_ERR_OOM : TADM_ERR_DEVICE, "pool (%zu bytes): %s", bytes,
                 hipGetErrorString(e));
   }
+  m->page_pools.push_back(p);
   *out = p;
   return TADM_OK;
 }
@@ -1505,6 +1521,8 @@ tadm_status tadm_pool_destroy(tadm_pool* pool) {
   (void)hipDeviceSynchronize();
   (void)hipFree(pool->data);
   (void)hipFree(pool->scale);
+  auto& all = pool->model->page_pools;
+  all.erase(std::remove(all.begin(), all.end(), pool), all.end());
   delete pool;
   return TADM_OK;
 }

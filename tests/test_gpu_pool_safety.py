@@ -12,7 +12,7 @@ tadm = pytest.importorskip("paper_2609_37924_amd")
 if not torch.cuda.is_available():
     pytest.skip("no GPU", allow_module_level=True)
 
-from test_gpu_pages import bounds  # noqa: E402
+from test_gpu_pages import bounds, i32, window  # noqa: E402
 from test_gpu_pooled import World  # noqa: E402
 from helpers import dev  # noqa: E402
 
@@ -165,3 +165,53 @@ def test_forks_under_capture_are_refused():
         for x in (root, kid):
             tadm.tadm_context_destroy(x)
         assert tadm.tadm_pool_free_pages(w.pool) == 40
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16 128"])
+def test_operators_on_the_rows_of_a_context(kind):
+    """Reading and attending work on a pool's pages with a context's rows; appending is refused, also to a part of
+    the table, and neither the context nor a fork that shares its pages changes.  A table of the program's own,
+    on pages that no context holds, can be appended to beside them."""
+    with World(kind) as w:
+        first, ctx = w.context(), w.context()
+        w.append(first, w.tokens(70, 1))
+        w.append(ctx, w.tokens(150, 2))
+        kid = tadm.tadm_context_fork(ctx, [0, 1])
+        before = w.read(ctx)
+        p, r = tadm.tadm_pool_pages(w.pool), tadm.tadm_context_rows(ctx)
+        H, hk, dh, n = w.cfg["n_heads"], w.cfg["n_kv_heads"], w.cfg["head_dim"], 6
+        name = "f32" if w.dt == torch.float32 else "bf16"
+        k, vt = window(np.random.default_rng(3), w.B, hk, 64, dh, name, 9.0)
+        q, kd, vd = torch.randn(w.B, H, n, dh, device=dev()).to(w.dt), k.to(dev()), vt.to(dev())
+        work = torch.empty(max(16, tadm.tadm_pages_attend_work(w.m, r, n)), dtype=torch.uint8, device=dev())
+        for layer in range(w.layers):
+            k2, v2 = torch.zeros(w.B, hk, 192, dh, dtype=w.dt, device=dev()), torch.zeros(w.B, hk, dh, 192, dtype=w.dt, device=dev())
+            tadm.tadm_pages_read(w.m, p, layer, r, k2, v2, 192)
+            K, V = before[layer]
+            assert np.array_equal(k2[:, :, :150].double().cpu().numpy(), K)
+            assert np.array_equal(v2[..., :150].transpose(2, 3).double().cpu().numpy(), V)
+            o = torch.zeros(w.B, n, H * dh, dtype=w.dt, device=dev())
+            tadm.tadm_pages_attend(w.m, p, layer, r, q, n, kd, vd, 64, o, None, work)
+            for b in range(w.B):
+                qb = q[b].double().cpu().numpy()
+                Kb = np.concatenate([K[b], k[b, :, :n].double().numpy()], 1)
+                Vb = np.concatenate([V[b], vt[b, :, :, :n].double().numpy().transpose(0, 2, 1)], 1)
+                ref, _ = P.attend(qb, Kb, Vb)
+                to, _ = bounds(name, qb, Kb, Vb)
+                assert np.all(np.abs(o[b].double().cpu().numpy().reshape(n, H, dh) - ref) <= to)
+        for skip, length in ((0, 150), (0, 40), (0, 192), (7, 0), (13, 0)):
+            part = tadm.tadm_context_rows(ctx)
+            part.table_dev, part.len = part.table_dev + 4 * skip, length
+            part.B, part.max_pages = (2, 7) if skip == 0 else (1, 14 - skip)
+            with pytest.raises(tadm.TadmError, match="tadm_context_append") as e:
+                tadm.tadm_pages_append(w.m, p, 0, part, kd, vd, 8, 64)
+            assert e.value.status == tadm.TADM_ERR_STATE
+        # the lowest ids that are free: behind the held ones after a compaction
+        tadm.tadm_pool_compact(w.pool)
+        held = 40 - tadm.tadm_pool_free_pages(w.pool)
+        mine = i32([[held], [held + 1]])
+        tadm.tadm_pages_append(w.m, p, 0, tadm.page_rows(mine, 0), kd, vd, 64, 64)
+        for x in (ctx, kid):
+            assert all(np.array_equal(a, b) for u, v in zip(before, w.read(x)) for a, b in zip(u, v))
+        for x in (first, ctx, kid):
+            tadm.tadm_context_destroy(x)
