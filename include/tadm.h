@@ -281,7 +281,9 @@ tadm_status tadm_context_create_pooled(tadm_model* m, tadm_pool* pool, int32_t B
  * src must be a pooled context and the call is not captured (TADM_ERR_STATE otherwise). */
 tadm_status tadm_context_fork(const tadm_context* src, const int32_t* rows, int32_t B, tadm_context** out);
 /* Drops the positions [len, tadm_context_length) of any context; a pooled one gives back the
- * pages that hold none of the others. */
+ * pages that hold none of the others.  A page that it keeps in part keeps its scale, and its codes
+ * stay as the dropped positions left them: where those had raised the scale, the ones that remain
+ * are rounded to it, and so are those appended next.  At whole pages nothing is left of what was dropped. */
 tadm_status tadm_context_truncate(tadm_context* ctx, int32_t len);
 /* The rows of a pooled context for the operators above (valid until it is destroyed; len as of now).
  * Behind the context's pages the table has absent ones. */

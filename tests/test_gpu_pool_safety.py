@@ -13,7 +13,7 @@ if not torch.cuda.is_available():
     pytest.skip("no GPU", allow_module_level=True)
 
 from test_gpu_pages import bounds, i32, window  # noqa: E402
-from test_gpu_pooled import World  # noqa: E402
+from test_gpu_pooled import World, same  # noqa: E402
 from helpers import dev  # noqa: E402
 
 
@@ -212,6 +212,64 @@ def test_operators_on_the_rows_of_a_context(kind):
         mine = i32([[held], [held + 1]])
         tadm.tadm_pages_append(w.m, p, 0, tadm.page_rows(mine, 0), kd, vd, 64, 64)
         for x in (ctx, kid):
-            assert all(np.array_equal(a, b) for u, v in zip(before, w.read(x)) for a, b in zip(u, v))
+            assert same(before, w.read(x))
         for x in (first, ctx, kid):
             tadm.tadm_context_destroy(x)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16 64"])
+def test_a_rollback_to_whole_pages_leaves_no_trace(kind):
+    """Positions appended and dropped again at a page's end, then others: reads and runs bit for bit as a context that
+    never had them."""
+    with World(kind) as w:
+        a, direct = w.context(), w.context()
+        first, last, z = w.tokens(64, 1), w.tokens(36, 2), w.tokens(12, 3)
+        for x in (a, direct):
+            w.append(x, first)
+        w.append(a, w.tokens(30, 4))
+        w.append(a, w.tokens(90, 5))
+        tadm.tadm_context_truncate(a, 64)
+        for x in (a, direct):
+            w.append(x, last)
+        assert same(w.read(a), w.read(direct))
+        assert torch.equal(w.step(a, z), w.step(direct, z))
+        for x in (a, direct):
+            tadm.tadm_context_destroy(x)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16 64", "bf16 128"])
+@pytest.mark.parametrize("keep, shared", [(70, False), (70, True), (127, True), (65, False)])
+def test_a_rollback_inside_a_page(kind, keep, shared):
+    """130 positions, cut inside the second page, then 20 others: layer 0, whose K, V depend on tokens and positions
+    alone, holds what the page oracle makes of a plain context's K, V (the kept page's scale and rounding
+    included).  A fork on the same pages reads as before, and, cut and continued like the other, reads alike."""
+    with World(kind) as w:
+        x, plain = w.context(), tadm.tadm_context_create(w.m, w.B, 448)
+        hk, dh = w.cfg["n_kv_heads"], w.cfg["head_dim"]
+        pages = [P.Pages(np.zeros((3, 1, hk, 2, 64 * dh), np.uint8), np.ones((3, 1, hk, 2))) for _ in range(w.B)]
+
+        def append(at, tok):
+            for c in (x, plain):
+                w.append(c, tok)
+            k, v = w.read(plain)[0]
+            for b in range(w.B):
+                pages[b].append(0, [0, 1, 2], at, k[b][:, at:], v[b][:, at:])
+
+        append(0, w.tokens(130, 1))
+        whole, kid = w.read(x), tadm.tadm_context_fork(x, [0, 1]) if shared else None
+        for c in (x, plain):
+            tadm.tadm_context_truncate(c, keep)
+        append(keep, w.tokens(20, 2))
+        got = w.read(x)
+        for b in range(w.B):
+            K, V, _ = pages[b].read(0, [0, 1, 2], keep + 20)
+            assert np.array_equal(got[0][0][b], K) and np.array_equal(got[0][1][b], V), b
+        if shared:
+            assert same(whole, w.read(kid))
+            tadm.tadm_context_truncate(kid, keep)
+            w.append(kid, w.tokens(20, 2))
+            assert same(got, w.read(kid)) and same(got, w.read(x))
+            tadm.tadm_context_destroy(kid)
+        for c in (x, plain):
+            tadm.tadm_context_destroy(c)
+        assert tadm.tadm_pool_free_pages(w.pool) == 40
