@@ -209,7 +209,8 @@ typedef struct {
  * largest finite magnitude of the new values: e = the least exponent with M <= 448 2^e,
  * in [-110, 120]; where the page holds earlier positions of the row the scale becomes
  * the larger of the present one and 2^e, and their codes are rounded again if it grew.
- * code(x) = x / scale rounded to nearest even; infinities and NaN become the NaN code.
+ * code(x) = x / scale rounded to nearest even (at e = 120 to at most 240, the largest code
+ * whose value is finite); infinities and NaN become the NaN code.
  * Codes of other positions stay as they are, and so do the rows' lengths (the caller
  * advances them).  No page may be written twice in a call, by two rows or by one.  The rows of
  * a pooled context (tadm_context_rows) are not for appending (TADM_ERR_STATE): its pages may be

@@ -9,6 +9,7 @@ import numpy as np
 
 PAGE = 64
 E_MIN, E_MAX = -110, 120
+LAST = 240.0  # the largest code value at the scale 2^E_MAX: the next would stand for 2^128
 
 
 def _positive():
@@ -84,7 +85,10 @@ class Pages:
                             at[:a] = encode(decode(at[:a]) * (old / scale))
                         scale = max(scale, old)
                     with np.errstate(invalid="ignore"):
-                        at[a:b] = encode(new / scale)
+                        y = new / scale
+                        if scale == 2.0 ** E_MAX:
+                            y = np.where(np.isfinite(y), np.clip(y, -LAST, LAST), y)
+                        at[a:b] = encode(y)
                     self.scales[page, layer, h, s] = scale
 
     def read(self, layer, ids, length):

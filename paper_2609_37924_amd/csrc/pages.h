@@ -11,8 +11,10 @@
 namespace tadm {
 
 constexpr int PAGE = 64;
-// exponents a scale may have: every value of a code is a normal bf16
+// exponents a scale may have: every value of a code is a normal bf16, at the largest of the codes up
+// to 240, where append stops (the next, 256, would be 2^128)
 constexpr int PAGE_E_MIN = -110, PAGE_E_MAX = 120;
+constexpr float PAGE_SCALE_MAX = 0x1p120f;
 
 // One layer of a page set: page p, head h at data + p * page_bytes + h * 128 * dh, its two
 // scales at scale + p * page_scales + 2 h.

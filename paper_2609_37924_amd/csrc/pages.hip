@@ -4,8 +4,8 @@
 // e = the least exponent with M <= 448 2^e (448 is the largest e4m3), cut to [-110, 120]; a
 // page that holds earlier positions of the row keeps the larger of its scale and 2^e, and if
 // it grew its codes are rounded again to the new scale.  code(x) = x 2^-e rounded to nearest
-// even; values that are not finite get the NaN code.  A power of two costs no precision: the
-// codes are floating point, and 2^-e x is exact.
+// even, at e = 120 at most 240, so that what is read back is finite; values that are not finite get the
+// NaN code.  A power of two costs no precision: the codes are floating point, and 2^-e x is exact.
 #include "common.h"
 #include "pages.h"
 
@@ -76,6 +76,12 @@ __device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d, f
 }
 __device__ __forceinline__ uint8_t code_of(float x, float inv) {
   return (uint8_t)(__builtin_amdgcn_cvt_pk_fp8_f32(x * inv, 0.f, 0, false) & 255);
+}
+// Four codes of the scale 2^120 with 256 (0x78), the only one above 240 that a finite number rounds to, taken to 240:
+// of 0x80 less the difference of two codes without signs, bit 7 is set where they are equal.
+__device__ __forceinline__ uint32_t capped(uint32_t w) {
+  const uint32_t d = (w & 0x7f7f7f7fu) ^ 0x78787878u;
+  return w - (((0x80808080u - d) & 0x80808080u) >> 7);
 }
 __device__ __forceinline__ float value_of(uint8_t c) { return __builtin_amdgcn_cvt_f32_fp8((int)c, 0); }
 
@@ -161,6 +167,7 @@ __global__ __launch_bounds__(256) void append_kernel(PageLayer p, PageRows r, co
     const bool grown = lo > 0 && s > old[side];  // the codes of the earlier places change
     if (lo > 0 && !grown) s = old[side];
     const float inv = 1.f / s, f = old[side] * inv;
+    const bool at_top = __builtin_amdgcn_readfirstlane(__float_as_int(s)) == __float_as_int(PAGE_SCALE_MAX);
     auto again = [&](uint8_t b) { return (uint8_t)(__builtin_amdgcn_cvt_pk_fp8_f32(value_of(b) * f, 0.f, 0, false) & 255); };
     if (whole) {
 #pragma unroll
@@ -175,6 +182,9 @@ __global__ __launch_bounds__(256) void append_kernel(PageLayer p, PageRows r, co
 #pragma unroll
         for (int e = 0; e < 4; ++e)
           w[e] = codes4(v.get(4 * e), v.get(4 * e + 1), v.get(4 * e + 2), v.get(4 * e + 3), inv);
+        if (at_top)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) w[e] = capped(w[e]);
         if (!all) {
           uint32_t had[4];
           *reinterpret_cast<uint4*>(had) = *reinterpret_cast<const uint4*>(c + 16 * u);
@@ -196,10 +206,10 @@ __global__ __launch_bounds__(256) void append_kernel(PageLayer p, PageRows r, co
           *at = again(*at);
         }
       for (int i = threadIdx.x; i < m * dh; i += 256) {
-        if (side == 0)
-          c[lo * dh + i] = code_of(f32_of(ks[lo * dh + i]), inv);
-        else
-          c[(i / m) * PAGE + lo + i % m] = code_of(f32_of(vs[(size_t)(i / m) * cap + lo + i % m]), inv);
+        const float y = f32_of(side == 0 ? ks[lo * dh + i] : vs[(size_t)(i / m) * cap + lo + i % m]);
+        const uint8_t b = code_of(y, inv);
+        uint8_t* at = side == 0 ? c + lo * dh + i : c + (i / m) * PAGE + lo + i % m;
+        *at = at_top ? (uint8_t)capped(b) : b;
       }
     }
     if (threadIdx.x == 0) scale[side] = s;

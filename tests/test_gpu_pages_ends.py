@@ -1,0 +1,60 @@
+"""The page operators at the ends of their ranges, on the GPU against the float64 oracle."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import pages as P
+
+pytestmark = pytest.mark.gpu
+
+tadm = pytest.importorskip("paper_2609_37924_amd")
+
+if not torch.cuda.is_available():
+    pytest.skip("no GPU", allow_module_level=True)
+
+from test_gpu_pages import DT, cap_of, i32, model, to_gpu  # noqa: E402
+from test_pages_ends import TOPS  # noqa: E402
+
+
+# ------------------------------------------------------------------ append, read
+@pytest.mark.parametrize("dtype, dh", [("f32", 4), ("f32", 20), ("bf16", 64), ("bf16", 128)])
+@pytest.mark.parametrize("length, n", [(0, 64), (3, 15), (5, 1), (0, 70), (40, 30), (64, 16)])
+def test_the_largest_values(dtype, dh, length, n):
+    """Codes and scales as the oracle's, and every finite value reads back finite: values up to the largest of the
+    type, beside infinities and NaN, into empty pages and behind positions whose scale grows or stays 2^120."""
+    Hkv, cap = 2, cap_of(n)
+    last = (length + n - 1) // 64 + 1
+    pages = P.Pages(np.zeros((4, 1, Hkv, 2, 64 * dh), np.uint8), np.ones((4, 1, Hkv, 2)))
+    rng = np.random.default_rng(dh + n)
+    x = rng.normal(size=(1, Hkv, cap, dh)) * 1e37
+    for t, top in enumerate(TOPS):
+        x[0, t % Hkv, t * 13 % n, t % dh] = top * (-1) ** t
+    x[0, 0, n - 1, 0], x[0, 1, n // 2, 1], x[0, 1, 0, 2] = np.inf, -np.inf, np.nan
+    most = torch.finfo(DT[dtype]).max
+    k = torch.from_numpy(np.where(np.isfinite(x), np.clip(x, -most, most), x)).to(DT[dtype])
+    v = torch.flip(k, (1,))
+    data, scale, p = to_gpu(pages)
+    m = model(dtype, Hkv, Hkv, dh)
+    try:
+        t = i32([[2, 0, 3]])
+        steps = [(0, k[:, :, :length], v[:, :, :length])] if length else []  # as many of the same values before
+        steps.append((length, k[:, :, :n], v[:, :, :n]))
+        for at, a, b in steps:
+            new, c = a.shape[2], cap_of(a.shape[2])
+            kd, vd = torch.zeros(1, Hkv, c, dh, dtype=DT[dtype]), torch.zeros(1, Hkv, dh, c, dtype=DT[dtype])
+            kd[:, :, :new], vd[..., :new] = a, b.transpose(2, 3)
+            kd, vd = kd.cuda(), vd.cuda()
+            tadm.tadm_pages_append(m, p, 0, tadm.page_rows(t, at), kd, vd, new, c)
+            pages.append(0, [2, 0, 3], at, a[0].double().numpy(), b[0].double().numpy())
+        assert np.array_equal(scale.cpu().double().numpy(), pages.scales)
+        got, ref = data.cpu().numpy(), pages.codes
+        both_nan = ((got & 0x7f) == 0x7f) & ((ref & 0x7f) == 0x7f)
+        assert np.array_equal(np.where(both_nan, 0, got), np.where(both_nan, 0, ref))
+        c = 64 * last
+        k2, v2 = torch.zeros(1, Hkv, c, dh, dtype=DT[dtype], device="cuda"), torch.zeros(1, Hkv, dh, c, dtype=DT[dtype], device="cuda")
+        tadm.tadm_pages_read(m, p, 0, tadm.page_rows(t, length + n), k2, v2, c)
+        for side, new in ((k2, k), (v2.transpose(2, 3), v)):
+            back = side[:, :, length:length + n].cpu()
+            assert torch.equal(back.isfinite(), new[:, :, :n].isfinite()) and not back.isinf().any()
+    finally:
+        tadm.tadm_model_destroy(m)
