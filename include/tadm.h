@@ -190,7 +190,9 @@ typedef struct {
  * written to it, and its positions take no part in attention.  The row holds
  * positions [0, len_b): len_b = len for every row, or with len_dev len_dev[b] cut to
  * [0, len].  Its window has n_b new tokens: n, or n_dev[b] cut to [0, n] (n is an
- * argument of each call; B * n, times n_heads in attention, is at most 2^26).  Lengths on
+ * argument of each call; B * n, times n_heads in attention, is at most 2^26, and a launch of
+ * attention, 256 threads of a float32 and 512 of a bf16 model at least for
+ * every row and K/V head, stays below 2^32).  Lengths on
  * the device are not read on the host, so a captured call serves any lengths within len
  * and n.  What a call writes may not overlap anything else that it reads or writes. */
 typedef struct {

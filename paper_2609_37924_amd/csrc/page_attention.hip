@@ -846,11 +846,12 @@ void start_join(const Args& a, hipStream_t s) {
     hipLaunchKernelGGL((join_kernel<T, 1>), dim3((unsigned)((cols + 7) / 8)), dim3(256), 0, s, a);
 }
 
-constexpr int NARROW_WAVES = 8;  // of a block with few columns
+constexpr int NARROW_WAVES = 8;  // of a block with few columns, as of one with many
 
-// Which kernel a call takes: columns of a block, and splits of the key axis.
+// Which kernel a call takes: columns of a block, splits of the key axis, and the blocks in all.
 struct Plan {
   int width, S;
+  long blocks;
 };
 
 // Measured on one MI355X, in us a call with everything around it:
@@ -870,7 +871,7 @@ Plan plan(DType dt, int B, int H, int Hkv, int dh, int L, int max_len) {
   const int ncol = H / Hkv * L;
   const int tiles = (max_len + PAGE - 1) / PAGE + (L + PAGE - 1) / PAGE;
   auto blocks = [&](int width) { return (long)B * Hkv * ((ncol + width - 1) / width); };
-  Plan p{16, 1};
+  Plan p{16, 1, 0};
   long most = tiles > 8 ? tiles / 4 : 1;  // float32
   if (dt == BF16 && ncol > 32) {
     p.width = blocks(128) < 256 ? 64 : 128;
@@ -882,13 +883,13 @@ Plan plan(DType dt, int B, int H, int Hkv, int dh, int L, int max_len) {
   long S = 256 / blocks(p.width);
   S = S < most ? S : most;
   p.S = S < 1 ? 1 : (int)S;
+  p.blocks = blocks(p.width) * p.S;
   return p;
 }
 
 template <typename K>
 void start(K kernel, const Args& a, const Plan& p, int threads, hipStream_t s) {
-  const long n = (long)a.r.B * a.p.Hkv * p.S * ((a.G * a.r.max_n + p.width - 1) / p.width);
-  launch_timed(kernel, dim3((unsigned)n), dim3(threads), 0, s, a);
+  launch_timed(kernel, dim3((unsigned)p.blocks), dim3(threads), 0, s, a);
 }
 
 template <int DH>
@@ -902,6 +903,10 @@ void start_bf16(const Args& a, const Plan& p, hipStream_t s) {
 }
 
 }  // namespace
+
+size_t page_attend_threads(DType dt, int B, int H, int Hkv, int dh, int L, int max_len) {
+  return (size_t)plan(dt, B, H, Hkv, dh, L, max_len).blocks * (dt == BF16 ? 64 * NARROW_WAVES : 256);
+}
 
 size_t page_attend_work(DType dt, int B, int H, int Hkv, int dh, int L, int max_len) {
   const Plan pl = plan(dt, B, H, Hkv, dh, L, max_len);

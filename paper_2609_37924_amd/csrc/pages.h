@@ -63,8 +63,10 @@ struct PageAttend {
   int H, cap;
   void* work;  // page_attend_work() bytes
 };
-// The bytes of partial results that a call of this shape keeps between its kernels, and the launch.
+// The bytes of partial results that a call of this shape keeps between its kernels, the threads of its
+// launch (below 2^32, or it fails), and the launch.
 size_t page_attend_work(DType dt, int B, int H, int Hkv, int dh, int L, int max_len);
+size_t page_attend_threads(DType dt, int B, int H, int Hkv, int dh, int L, int max_len);
 hipError_t page_attend(DType dt, const PageAttend& a, hipStream_t s);
 
 }  // namespace tadm

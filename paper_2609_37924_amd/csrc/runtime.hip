@@ -1363,12 +1363,22 @@ static tadm_status check_rows(const tadm_page_rows* r) {
   return TADM_OK;
 }
 
-// A window of n tokens and n queries of each for each of `heads` heads (0: not known yet): a launch's threads and
-// the positions of a row stay below 2^31.
+// A window of n tokens and n queries of each for each of `heads` heads (0: not known yet): the positions of a row
+// and the columns of attention stay below 2^31.
 static tadm_status check_window_size(const tadm_page_rows* rows, int n, int heads) {
   if (n < 1 || n > (1 << 26)) return fail(TADM_ERR_INVALID, "n=%d outside [1, 2^26]", n);
   if ((long)rows->B * n > (1 << 26) / std::max(heads, 1))
     return fail(TADM_ERR_INVALID, "%d rows of %d queries: too many in one call, which takes 2^26", rows->B, n);
+  return TADM_OK;
+}
+
+// Attention of such a window in the model's heads, within the threads of one launch.
+static tadm_status check_attend_size(const tadm_model* m, const tadm_page_rows* rows, int n) {
+  const tadm_config& c = m->cfg;
+  TRY(check_window_size(rows, n, c.n_heads));
+  if (page_attend_threads(m->dt, rows->B, c.n_heads, c.n_kv_heads, c.head_dim, n, rows->len) >> 32)
+    return fail(TADM_ERR_INVALID, "%d rows of %d K/V heads: too many in one call, whose launch takes 2^32 threads", rows->B,
+                c.n_kv_heads);
   return TADM_OK;
 }
 
@@ -1420,7 +1430,7 @@ tadm_status tadm_pages_append(tadm_model* m, const tadm_pages* p, int32_t layer,
 }
 
 size_t tadm_pages_attend_work(const tadm_model* m, const tadm_page_rows* rows, int32_t n) {
-  if (check_rows(rows) != TADM_OK || !m || check_window_size(rows, n, m->cfg.n_heads) != TADM_OK) return 0;
+  if (check_rows(rows) != TADM_OK || !m || check_attend_size(m, rows, n) != TADM_OK) return 0;
   return page_attend_work(m->dt, rows->B, m->cfg.n_heads, m->cfg.n_kv_heads, m->cfg.head_dim, n, rows->len);
 }
 
@@ -1435,7 +1445,7 @@ tadm_status tadm_pages_attend(tadm_model* m, const tadm_pages* p, int32_t layer,
     return fail(TADM_ERR_INVALID, "queries or output not aligned to 16 bytes");
   if (k_dev || vt_dev) TRY(check_window_kv(k_dev, vt_dev, n, cap));
   TRY(check_page_model(m, p));
-  TRY(check_window_size(rows, n, m->cfg.n_heads));
+  TRY(check_attend_size(m, rows, n));
   const size_t need = tadm_pages_attend_work(m, rows, n);
   if (need && (!work_dev || work_bytes < need || !aligned(work_dev, 16)))
     return fail(TADM_ERR_INVALID, "scratch of %zu bytes, %zu needed, aligned to 16", work_dev ? work_bytes : 0, need);

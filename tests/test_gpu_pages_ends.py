@@ -58,3 +58,30 @@ def test_the_largest_values(dtype, dh, length, n):
             assert torch.equal(back.isfinite(), new[:, :, :n].isfinite()) and not back.isinf().any()
     finally:
         tadm.tadm_model_destroy(m)
+
+
+# ------------------------------------------------------------------ attention
+def test_rows_beyond_a_launch():
+    """More rows and K/V heads than a launch has threads for are refused by name, before anything is read; at the
+    limit of rows fewer heads are not."""
+    m = model("bf16", 256, 256, 64)
+    few = model("bf16", 4, 2, 64)
+    try:
+        pages = P.Pages(np.zeros((1, 1, 256, 2, 64 * 64), np.uint8), np.ones((1, 1, 256, 2)))
+        data, scale, p = to_gpu(pages)
+        t = i32([[0]])
+        r = tadm.page_rows(t, 0)
+        r.B = 65535
+        q = torch.zeros(64, dtype=torch.bfloat16, device="cuda")
+        assert tadm.tadm_pages_attend_work(m, r, 1) == 0 and "2^32 threads" in tadm.last_error()
+        with pytest.raises(tadm.TadmError, match="2\\^32 threads") as e:
+            tadm.tadm_pages_attend(m, p, 0, r, q, 1, None, None, 0, q, None, None)
+        assert e.value.status == tadm.TADM_ERR_INVALID
+        refused = tadm.last_error()
+        r = tadm.page_rows(t, 64)
+        r.B = 65535
+        assert tadm.tadm_pages_attend_work(few, r, 256) == 0  # 2^26 queries, in more blocks than any card has at once
+        assert tadm.last_error() == refused
+    finally:
+        tadm.tadm_model_destroy(m)
+        tadm.tadm_model_destroy(few)
