@@ -248,8 +248,8 @@ def page_set(data, scale):
     n_pages, n_layers, heads, two, width = data.shape
     if two != 2 or width % PAGE or tuple(scale.shape) != (n_pages, n_layers, heads, 2):
         raise ValueError(f"pages of shape {tuple(data.shape)} with scales of shape {tuple(scale.shape)}")
-    if data.element_size() != 1 or not scale.is_floating_point() or scale.element_size() != 4:
-        raise ValueError("pages hold 8-bit codes and float32 scales")
+    if str(data.dtype) not in ("torch.uint8", "torch.float8_e4m3fn") or str(scale.dtype) != "torch.float32":
+        raise ValueError(f"pages hold uint8 or float8_e4m3fn codes and float32 scales, not {data.dtype} and {scale.dtype}")
     if not (data.is_contiguous() and scale.is_contiguous()):
         raise ValueError("pages and scales must be contiguous")
     return tadm_pages(data=ptr(data), scale=ptr(scale), n_pages=n_pages, n_layers=n_layers, n_kv_heads=heads,

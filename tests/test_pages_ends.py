@@ -37,3 +37,14 @@ def test_growing_to_the_last_scale():
     pages.append(0, [0], 1, np.full((1, 1, 4), F32_MAX), -x)
     k, v, _ = pages.read(0, [0], 2)
     assert np.array_equal(k[0], np.array([[224.0], [240.0]]).repeat(4, 1) * 2.0 ** 120) and np.array_equal(v[0, 1], -x[0, 0])
+
+
+def test_page_sets_of_other_types_are_refused():
+    """Codes in other 8-bit types would be taken for e4m3."""
+    tadm = pytest.importorskip("paper_2609_37924_amd")
+    scale = torch.zeros(4, 2, 3, 2)
+    for dt in (torch.float8_e5m2, torch.int8, torch.bool, torch.float8_e4m3fnuz):
+        with pytest.raises(ValueError, match="float8_e4m3fn codes"):
+            tadm.page_set(torch.zeros(4, 2, 3, 2, 64 * 16, dtype=dt), scale)
+    for dt in (torch.uint8, torch.float8_e4m3fn):
+        assert tadm.page_set(torch.zeros(4, 2, 3, 2, 64 * 16, dtype=dt), scale).head_dim == 16
