@@ -855,8 +855,12 @@ struct Plan {
 };
 
 // Measured on one MI355X, in us a call with everything around it:
-//  - Blocks of 128 columns, unless those of 64 are needed to give every CU one (4 rows x 256 tokens over 2 000
-//    positions, 16/4 heads x 128: 32 with 64 columns, 46 with 128; 16 rows x 128 over 1 024: 38 and 30).
+//  - Many columns: blocks of 128 or of 64, whichever needs less for its rounds of 256 blocks.  With 128 elements a key
+//    a round of 128 columns takes as long as one and a half of 64 (16 heads, over 1 000 positions, in
+//    rounds of 128 against of 64: 5 rows x 192 tokens, 1 : 1, 30.7 and 21.6; 10 x 100, 1 : 2, 28.2 and 37.9; 9 x 160,
+//    2 : 2, 59 and 41; 16 x 192, 2 : 3, 60.3 and 60.7; 12 x 320, 3 : 4, 93 and 85; 16 x 320, 3 : 5, 96 and 106);
+//    with 64, where a CU holds two of the narrower, as long as two (12 heads: 8 x 128, 1 : 1, 21.5 and 13.7; 16 x 128,
+//    1 : 2, 19.5 and 20.7; 16 x 256, 2 : 3, 39.3 and 32.5; 10 x 512, 2 : 4, 45 and 46; 15 x 340, 3 : 5, 62 and 52).
 //  - At most a block per CU in all: 16 tokens over 8 192 positions (256 blocks) take 81, and 95 in two splits;
 //    1 token over 131 000 29 in 64 splits of 4 blocks, 33 in 32, and 34 in 128.
 //  - Few columns: a split has two tiles of 128 or four of 64 elements a key, from 9 and 25 tiles on (1 token,
@@ -874,7 +878,8 @@ Plan plan(DType dt, int B, int H, int Hkv, int dh, int L, int max_len) {
   Plan p{16, 1, 0};
   long most = tiles > 8 ? tiles / 4 : 1;  // float32
   if (dt == BF16 && ncol > 32) {
-    p.width = blocks(128) < 256 ? 64 : 128;
+    auto rounds = [&](int width) { return (blocks(width) + 255) / 256; };
+    p.width = dh > 64 ? (3 * rounds(128) <= 2 * rounds(64) ? 128 : 64) : (2 * rounds(128) <= rounds(64) ? 128 : 64);
     most = tiles > 12 ? tiles / 4 : 1;
   } else if (dt == BF16) {
     p.width = ncol > 16 ? 32 : 16;

@@ -12,7 +12,7 @@ tadm = pytest.importorskip("paper_2609_37924_amd")
 if not torch.cuda.is_available():
     pytest.skip("no GPU", allow_module_level=True)
 
-from test_gpu_pages import DT, cap_of, i32, model, to_gpu  # noqa: E402
+from test_gpu_pages import DT, bounds, cap_of, i32, model, random_pages, run_attend, to_gpu, window  # noqa: E402
 from test_pages_ends import TOPS  # noqa: E402
 
 
@@ -85,3 +85,43 @@ def test_rows_beyond_a_launch():
     finally:
         tadm.tadm_model_destroy(m)
         tadm.tadm_model_destroy(few)
+
+
+def held_to_oracle(dtype, pages, table, spans, q, k, vt, o, lse, heads):
+    """Rows of an attention over layer 0 (a K/V head per query head), in some heads, and what lies behind each window."""
+    B, H, n, dh = q.shape
+    o, lse = o.double().cpu().numpy().reshape(B, n, H, dh), lse.double().cpu().numpy()
+    for b, (length, new) in enumerate(spans):
+        assert np.all(o[b, new:] == 7.0) and np.all(lse[b, :, new:] == 7.0), f"row {b}: padding was written"
+        for h in heads if new else ():
+            K, V, _ = P.Pages(pages.codes[:, :, h:h + 1].copy(), pages.scales[:, :, h:h + 1].copy()).read(0, table[b], length)
+            K = np.concatenate([K, k[b, h:h + 1, :new].double().numpy()], axis=1)
+            V = np.concatenate([V, vt[b, h:h + 1, :, :new].double().numpy().transpose(0, 2, 1)], axis=1)
+            qh = q[b, h:h + 1, :new].double().numpy()
+            ref, ref_lse = P.attend(qh, K, V)
+            to, tl = bounds(dtype, qh, K, V)
+            assert np.all(np.abs(o[b, :new, h:h + 1] - ref) <= to), (b, h)
+            assert np.all(np.abs(lse[b, h, :new] - ref_lse[0]) <= tl[0]), (b, h)
+
+
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("B, n", [(24, 33), (18, 64), (10, 100), (9, 160), (16, 192)])
+def test_more_blocks_than_compute_units(dh, B, n):
+    """One to three rounds of blocks of 64 and of 128 columns, their last columns empty or not, behind pages."""
+    rng = np.random.default_rng(B + dh)
+    H = Hkv = 16
+    spans = [([130, 64, 0, 200, 321][b % 5], [n, 1, n - 1, 0][b % 4]) for b in range(B)]
+    mp, cap = 6, cap_of(n)
+    pages = random_pages(rng, B * mp, 1, Hkv, dh)
+    table = rng.permutation(B * mp).reshape(B, mp)
+    q = torch.from_numpy(rng.normal(size=(B, H, n, dh))).to(torch.bfloat16)
+    k, vt = window(rng, B, Hkv, cap, dh, "bf16")
+    for b, (_, new) in enumerate(spans):
+        k[b, :, new:], vt[b, :, :, new:], q[b, :, new:] = float("nan"), float("nan"), float("nan")
+    data, scale, p = to_gpu(pages)
+    m = model("bf16", H, Hkv, dh)
+    try:
+        o, lse = run_attend(m, "bf16", p, 0, table, [a for a, _ in spans], [b for _, b in spans], mp * 64, q, k, vt, cap)
+    finally:
+        tadm.tadm_model_destroy(m)
+    held_to_oracle("bf16", pages, table, spans, q, k, vt, o, lse, (0, Hkv - 1))
