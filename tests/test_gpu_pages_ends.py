@@ -125,3 +125,56 @@ def test_more_blocks_than_compute_units(dh, B, n):
     finally:
         tadm.tadm_model_destroy(m)
     held_to_oracle("bf16", pages, table, spans, q, k, vt, o, lse, (0, Hkv - 1))
+
+
+@pytest.mark.parametrize("dtype, Hkv, dh, spans, n", [
+    # bf16: blocks of 128 and of 64 columns, one and several splits
+    ("bf16", 8, 128, [(0, 1000), (100, 999), (64, 513), (0, 0), (300, 1), (37, 960), (128, 1000), (1, 640)], 1000),
+    ("bf16", 8, 64, [(0, 1000), (100, 999), (64, 513), (0, 0), (300, 1), (37, 960), (128, 1000), (1, 640)], 1000),
+    ("bf16", 2, 128, [(0, 520), (200, 577)], 577),
+    ("bf16", 2, 64, [(0, 520), (200, 577)], 577),
+    ("bf16", 1, 128, [(0, 1536)], 1536),
+    ("f32", 2, 16, [(0, 600), (333, 517)], 600),
+])
+def test_windows_of_a_prompt(dtype, Hkv, dh, spans, n):
+    """Windows of many tiles of their own keys, as appending a prompt has them, behind pages and without."""
+    rng = np.random.default_rng(n + dh)
+    B, mp, cap = len(spans), 6, cap_of(n)
+    pages = random_pages(rng, B * mp, 1, Hkv, dh)
+    table = rng.permutation(B * mp).reshape(B, mp)
+    q = torch.from_numpy(rng.normal(size=(B, Hkv, n, dh))).to(DT[dtype])
+    k, vt = window(rng, B, Hkv, cap, dh, dtype)
+    for b, (_, new) in enumerate(spans):
+        k[b, :, new:], vt[b, :, :, new:], q[b, :, new:] = float("nan"), float("nan"), float("nan")
+    data, scale, p = to_gpu(pages)
+    m = model(dtype, Hkv, Hkv, dh)
+    try:
+        o, lse = run_attend(m, dtype, p, 0, table, [a for a, _ in spans], [b for _, b in spans], mp * 64, q, k, vt, cap)
+    finally:
+        tadm.tadm_model_destroy(m)
+    held_to_oracle(dtype, pages, table, spans, q, k, vt, o, lse, sorted({0, Hkv - 1}))
+
+
+@pytest.mark.parametrize("length, n", [(9000, 70), (8500, 128)])
+def test_blocks_of_128_columns_over_many_tiles(length, n):
+    """64 elements a key, enough rows for one split: a wave walks more tiles than a batch of 64.  The rows share
+    their pages and queries, so all equal the first, which is held to the oracle in two heads."""
+    rng = np.random.default_rng(length)
+    Hkv, dh, B, mp = 16, 64, 16, -(-length // 64)
+    pages = random_pages(rng, mp + 1, 1, Hkv, dh)
+    table = np.tile(rng.permutation(mp + 1)[:mp], (B, 1))
+    q = torch.from_numpy(rng.normal(size=(1, Hkv, n, dh))).to(torch.bfloat16).expand(B, -1, -1, -1).contiguous()
+    data, scale, p = to_gpu(pages)
+    m = model("bf16", Hkv, Hkv, dh)
+    try:
+        o, lse = run_attend(m, "bf16", p, 0, table, [length] * B, [n] * B, length, q, None, None, 64)
+    finally:
+        tadm.tadm_model_destroy(m)
+    assert torch.equal(o, o[:1].expand_as(o)) and torch.equal(lse, lse[:1].expand_as(lse))
+    o, lse = o[0].double().cpu().numpy().reshape(n, Hkv, dh), lse[0].double().cpu().numpy()
+    for h in (0, Hkv - 1):
+        K, V, _ = P.Pages(pages.codes[:, :, h:h + 1].copy(), pages.scales[:, :, h:h + 1].copy()).read(0, table[0], length)
+        qh = q[0, h:h + 1].double().numpy()
+        ref, ref_lse = P.attend(qh, K, V)
+        to, tl = bounds("bf16", qh, K, V)
+        assert np.all(np.abs(o[:, h:h + 1] - ref) <= to) and np.all(np.abs(lse[h] - ref_lse[0]) <= tl[0])

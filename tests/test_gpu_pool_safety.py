@@ -14,6 +14,7 @@ if not torch.cuda.is_available():
 
 from test_gpu_pages import bounds, i32, window  # noqa: E402
 from test_gpu_pooled import World, same  # noqa: E402
+from test_gpu_pooled import test_passes_on_a_pooled_context as passes  # noqa: E402
 from helpers import dev  # noqa: E402
 
 
@@ -273,3 +274,11 @@ def test_a_rollback_inside_a_page(kind, keep, shared):
         for c in (x, plain):
             tadm.tadm_context_destroy(c)
         assert tadm.tadm_pool_free_pages(w.pool) == 40
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16 64", "bf16 128"])
+@pytest.mark.parametrize("pieces", [(300, 100), (413,)])
+def test_passes_behind_a_prompt(kind, pieces):
+    """Prompts of several tiles appended at once, and once more behind them, then a refresh and a step, against the
+    oracle."""
+    passes(kind, pieces)
