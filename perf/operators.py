@@ -312,9 +312,8 @@ def _handle(state):
         cfg = dict(dtype=c["dtype"], vocab=64, d_model=64, n_heads=c["heads"], n_kv_heads=c["kv_heads"],
                    head_dim=c["head_dim"], d_ffn=64, ffn_kind="gelu", n_shared=0, n_anchor=1, n_denoise=1,
                    fusion_kind="gated_mlp", rms_eps=1e-6, ln_eps=1e-5, rope_theta=10000.0)
-        m = tadm.tadm_model_create(tadm.make_config(cfg, max_batch=16, max_seq=1024))
-        tadm.tadm_set_stream(m, torch.cuda.current_stream().cuda_stream)
-        _models[key] = m
+        _models[key] = tadm.tadm_model_create(tadm.make_config(cfg, max_batch=16, max_seq=1024))
+    tadm.tadm_set_stream(_models[key], torch.cuda.current_stream().cuda_stream)  # the caller's, call by call
     return tadm, _models[key]
 
 
