@@ -301,7 +301,8 @@ def _plain_read(state):
 
 
 # ------------------------------------------------------------ the framework's calls
-_models = {}  # one model handle per head layout, as a serving program has
+_models = {}   # one model handle per head layout, as a serving program has
+_streams = {}  # and the stream that each works on
 
 
 def _handle(state):
@@ -313,7 +314,10 @@ def _handle(state):
                    head_dim=c["head_dim"], d_ffn=64, ffn_kind="gelu", n_shared=0, n_anchor=1, n_denoise=1,
                    fusion_kind="gated_mlp", rms_eps=1e-6, ln_eps=1e-5, rope_theta=10000.0)
         _models[key] = tadm.tadm_model_create(tadm.make_config(cfg, max_batch=16, max_seq=1024))
-    tadm.tadm_set_stream(_models[key], torch.cuda.current_stream().cuda_stream)  # the caller's, call by call
+    stream = torch._C._cuda_getCurrentRawStream(state["data"].get_device())  # the caller's, without a Stream object
+    if _streams.get(key) != stream:
+        tadm.tadm_set_stream(_models[key], stream)
+        _streams[key] = stream
     return tadm, _models[key]
 
 
