@@ -18,19 +18,12 @@ def cases():
 
 
 def test_calls_follow_the_current_stream(monkeypatch):
-    """One handle per head layout, its stream set anew by every call."""
-    mod, made, streams = cases(), [], []
-
-    class Stream:
-        cuda_stream = 11
-
+    """One handle per head layout, its stream set where the current one is another."""
+    mod, made, streams, now = cases(), [], [], [11]
     monkeypatch.setattr(tadm, "tadm_model_create", lambda cfg: made.append(cfg) or len(made))
     monkeypatch.setattr(tadm, "tadm_set_stream", lambda m, s: streams.append((m, s)))
-    monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: Stream)
-    block, small = (dict(case=next(c for c in mod.listed() if c["heads"] == h)) for h in (16, 12))
-    assert mod._handle(block)[1] == 1
-    Stream.cuda_stream = 12
-    assert mod._handle(block)[1] == 1 and mod._handle(small)[1] == 2
-    Stream.cuda_stream = 13
-    assert mod._handle(block)[1] == 1
-    assert len(made) == 2 and streams == [(1, 11), (1, 12), (2, 12), (1, 13)]
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: now[0], raising=False)
+    block, small = (dict(case=next(c for c in mod.listed() if c["heads"] == h), data=torch.zeros(1)) for h in (16, 12))
+    for now[0], state, m in ((11, block, 1), (11, block, 1), (12, block, 1), (12, small, 2), (13, block, 1), (11, block, 1)):
+        assert mod._handle(state)[1] == m
+    assert len(made) == 2 and streams == [(1, 11), (1, 12), (2, 12), (1, 13), (1, 11)]
