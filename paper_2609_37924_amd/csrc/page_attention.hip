@@ -82,8 +82,8 @@ __device__ __forceinline__ int key_of(int i, int grp, int j) {
 
 // One tile of a strip's softmax, in base 2.  s[i][j]: the score of key_of(i, grp, j), unscaled; on return
 // its probability relative to a reference m of the column, that moves only when a score of the
-// tile exceeds it by more than 2^8: until then the probabilities stay below 256, and neither
-// the sum l nor O need rescaling.  So most tiles need no maximum over the lanes of a column.
+// tile exceeds it by more than 8 (in base 2): until then the probabilities stay at 2^8 or below, and
+// neither the sum l nor O need rescaling.  So most tiles need no maximum over the lanes of a column.
 // M_NONE, below every finite score, is the reference before the first.
 constexpr float M_NONE = -3.402823466e38f;
 template <bool RUN, int NB>
@@ -341,8 +341,12 @@ __device__ __forceinline__ float at_lane(float v, int lane) {
   return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane));
 }
 
-// Probabilities are rounded to bf16 here, for the bf16 products (at most 2^-8 of each, like the rounding of the
-// result; the sum l has them unrounded): float32 products are sixteen times slower.
+// Probabilities are rounded to bf16 here (at most 2^-8 of each, like the rounding of the result; the sum l has
+// them unrounded), as attention over a bf16 context rounds them: against 64 bits the result's error is 0.0021 to
+// 0.0023 of its norm where rounding the result alone leaves 0.0017.  float32 products are sixteen times
+// slower.  f16 ones, as fast, would round a probability eight times finer, but their V would have to be f16 too: the
+// window's bf16 values have a range that it lacks, and so have the scales (2^-110 to 2^120), which would
+// have to meet the probabilities (out of their range as well) or, tile by tile, every element of O.
 // Probabilities of a tile as the operand of O^T = V^T P^T: k index 8 grp + j of product c is the key of
 // score row 4 grp + j % 4 of block 2 c + j / 4.
 __device__ __forceinline__ void p_operand(const f32x4 (&s)[4], bf16x8 (&p)[2]) {
@@ -414,7 +418,7 @@ __device__ __forceinline__ void window_tile(const Args& a, const Block& x, int w
 // Bound by the pages' bytes: no wave reads what another does, so LDS would only add a way, and
 // with a tile on its way per wave eight waves keep 128 KB a CU outstanding (128 elements a key).  16 tokens
 // over up to 8 192 positions, 32/16 heads x 128 (412 MB): 81 us, 5.1 TB/s, the rate of a copy of 1 GiB
-// on the same card (blocks of four waves took 101 where those of eight took 85).  1 token over 131 071
+// on the same card (row kernels that write less reach 6.0) (blocks of four waves took 101 where those of eight took 85).  1 token over 131 071
 // positions, 16/4 heads x 128 (134 MB): 32 with the join of its splits, 26 at the copy's rate.  1 token over
 // 200 positions: 7.7, of which an empty launch takes 3.6; the rest is loads that wait for one
 // another (lengths and table, scales, codes, the window) and the join of the waves.
@@ -530,8 +534,8 @@ __device__ __forceinline__ int swizzle(int row) {
 // LDS beside the matrix products.
 //
 // Bound by the half steps, the products' against the exponentials': 4 rows of 256 tokens over 16 384
-// positions, 32/16 heads x 128 (279 Gflop): 286 us, 979 TFLOP/s; at the 1 318 of a large library
-// product 212.  A half step of products takes 2 060 to 2 340 cycles for 1 024 of matrix instructions a
+// positions, 32/16 heads x 128 (279 Gflop): 279 to 286 us, 979 to 1 000 TFLOP/s; at the 1 318 of a large
+// library product 212.  A half step of products takes 2 060 to 2 340 cycles for 1 024 of matrix instructions a
 // wave, one of exponentials 1 050 to 1 600, both stretched by the other group's instructions.
 // Both groups at the same step took 331 where turns took 307, K placed beside the exponentials 296 where beside
 // the products 290, a second tile ahead in registers 327 to 353.
@@ -862,7 +866,9 @@ struct Plan {
 //    with 64, where a CU holds two of the narrower, as long as two (12 heads: 8 x 128, 1 : 1, 21.5 and 13.7; 16 x 128,
 //    1 : 2, 19.5 and 20.7; 16 x 256, 2 : 3, 39.3 and 32.5; 10 x 512, 2 : 4, 45 and 46; 15 x 340, 3 : 5, 62 and 52).
 //  - At most a block per CU in all: 16 tokens over 8 192 positions (256 blocks) take 81, and 95 in two splits;
-//    1 token over 131 000 29 in 64 splits of 4 blocks, 33 in 32, and 34 in 128.
+//    1 token over 131 000 29 in 64 splits of 4 blocks, 33 in 32, and 34 in 128.  All with 128 elements a key; with
+//    64 a CU has room for two blocks, and with 129 to 255 blocks a part of the chip is left empty: neither was
+//    tried with more splits.
 //  - Few columns: a split has two tiles of 128 or four of 64 elements a key, from 9 and 25 tiles on (1 token,
 //    16/4 heads x 128, over 8 000 positions: 12.7 in 16 splits, 10.7 in 32 and 64; over 1 000, 13.7 in one and
 //    10.2 in 8; over 300, 8.5 in one and 10.2 in two;

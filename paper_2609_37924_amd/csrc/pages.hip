@@ -90,10 +90,10 @@ __device__ __forceinline__ float value_of(uint8_t c) { return __builtin_amdgcn_c
 // search for the maximum and the rounding, so that the window is read once.  A unit
 // that holds other positions as well keeps theirs.
 //
-// Bound by HBM for prompts: 1 024 tokens in 4 rows, 16 heads x 128, from position 37 on (50 MB): 17.2 us, 2.9 TB/s,
-// against 9.8 at the rate of a large copy; every block waits for the whole of its window before it
-// may round, and keys that start inside a page make the unit loads of V^T straddle lines.  With
-// single elements throughout 48.7.  One token in each of 16 rows: 5.1, of which an empty launch takes 3.6.
+// HBM's for prompts, but not at its rate: 1 024 tokens in 4 rows, 16 heads x 128, from position 37 on (50 MB): 17.2 us,
+// 2.9 TB/s, against 9.8 at the rate of a large copy.  Every block waits for the whole of its window before it
+// may round, and keys that start inside a page make the unit loads of V^T straddle lines, each of which two
+// pages read; which of these costs what was not measured.  With single elements throughout 48.7.  One token in each of 16 rows: 5.1, of which an empty launch takes 3.6.
 template <class T>
 __global__ __launch_bounds__(256) void append_kernel(PageLayer p, PageRows r, const T* k, const T* vt, int cap) {
   __shared__ float red[2][4];
@@ -280,7 +280,8 @@ struct CopyPairs {
 };
 
 // grid: x = 16 KB pieces of a page, y = pairs.  Bound by HBM: 96 pages of 46 layers of 16 heads x 128 (2.3 GB):
-// 420 us, 5.5 TB/s; 4 pages of 24 layers of 4 heads x 128 (12.6 MB): 6.7, of which an empty launch takes 3.6.
+// 420 us, 5.5 TB/s; 4 pages of 24 layers of 4 heads x 128 (12.6 MB): 6.7, an empty launch's 3.6 and 2.5 at the rate of a
+// large copy (with fewer bytes of arguments 6.9).
 __global__ __launch_bounds__(256) void copy_pages_kernel(uint8_t* data, float* scale, size_t page_bytes,
                                                          size_t page_scales, CopyPairs pairs) {
   const int src = pairs.src[blockIdx.y], dst = pairs.dst[blockIdx.y];
