@@ -215,8 +215,8 @@ typedef struct {
  * whose value is finite); infinities and NaN become the NaN code.
  * Codes of other positions stay as they are, and so do the rows' lengths (the caller
  * advances them).  No page may be written twice in a call, by two rows or by one.  The rows of
- * a pooled context (tadm_context_rows) are not for appending (TADM_ERR_STATE): its pages may be
- * shared, and tadm_context_append parts them. */
+ * a pooled context of the model (tadm_context_rows) are not for appending (TADM_ERR_STATE): its
+ * pages may be shared, and tadm_context_append parts them. */
 tadm_status tadm_pages_append(tadm_model* m, const tadm_pages* p, int32_t layer, const tadm_page_rows* rows,
                               const void* k_dev, const void* vt_dev, int32_t n, int32_t cap);
 /* Attention of a window over the rows' pages of one layer: for every query q_dev
@@ -258,7 +258,9 @@ tadm_status tadm_pool_destroy(tadm_pool* pool);
 /* Pages in all, and pages that no context holds (0 for NULL). */
 int32_t tadm_pool_size(const tadm_pool* pool);
 int32_t tadm_pool_free_pages(const tadm_pool* pool);
-/* The pool's arrays for the operators above; valid until tadm_pool_resize. */
+/* The pool's arrays for the operators above; valid until tadm_pool_resize.  They are for reading: what is on
+ * held pages is their contexts', and a page that none holds may be any context's at its next append.  Programs
+ * that write pages by themselves keep arrays of their own. */
 tadm_status tadm_pool_pages(const tadm_pool* pool, tadm_pages* out);
 /* Moves the held pages to the lowest ids, in the contexts' tables too (enqueued like any work; not under
  * graph capture: TADM_ERR_STATE). */

@@ -171,8 +171,8 @@ def test_forks_under_capture_are_refused():
 @pytest.mark.parametrize("kind", ["f32", "bf16 128"])
 def test_operators_on_the_rows_of_a_context(kind):
     """Reading and attending work on a pool's pages with a context's rows; appending is refused, also to a part of
-    the table, and neither the context nor a fork that shares its pages changes.  A table of the program's own,
-    on pages that no context holds, can be appended to beside them."""
+    the table, and neither the context nor a fork that shares its pages changes.  Rows and pages of the program's own
+    are appended to as ever."""
     with World(kind) as w:
         first, ctx = w.context(), w.context()
         w.append(first, w.tokens(70, 1))
@@ -207,11 +207,10 @@ def test_operators_on_the_rows_of_a_context(kind):
             with pytest.raises(tadm.TadmError, match="tadm_context_append") as e:
                 tadm.tadm_pages_append(w.m, p, 0, part, kd, vd, 8, 64)
             assert e.value.status == tadm.TADM_ERR_STATE
-        # the lowest ids that are free: behind the held ones after a compaction
-        tadm.tadm_pool_compact(w.pool)
-        held = 40 - tadm.tadm_pool_free_pages(w.pool)
-        mine = i32([[held], [held + 1]])
-        tadm.tadm_pages_append(w.m, p, 0, tadm.page_rows(mine, 0), kd, vd, 64, 64)
+        data = torch.zeros(2, 1, hk, 2, 64 * dh, dtype=torch.uint8, device=dev())
+        scale, table = torch.ones(2, 1, hk, 2, device=dev()), i32([[0], [1]])
+        tadm.tadm_pages_append(w.m, tadm.page_set(data, scale), 0, tadm.page_rows(table, 0), kd, vd, 64, 64)
+        assert (data != 0).any() and (scale != 1).all()
         for x in (ctx, kid):
             assert same(before, w.read(x))
         for x in (first, ctx, kid):
