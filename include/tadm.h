@@ -248,6 +248,34 @@ tadm_status tadm_pages_read(tadm_model* m, const tadm_pages* p, int32_t layer, c
 tadm_status tadm_pages_copy(tadm_model* m, const tadm_pages* p, const int32_t* src, const int32_t* dst,
                             int32_t n_copies);
 
+/* Tables kept on the device: rows take pages from a stack of free ones and give them back, without the host.  The
+ * free pages are id_dev[0, state_dev[0]), the next one taken at the back; size is the entries of id_dev and the
+ * pages in all; the other three words of state_dev are the calls' own, 0 at first.  A row uses the table entries
+ * [0, ceil(len_b / TADM_PAGE)); its n_b new tokens, at positions [len_b, len_b + n_b), need the entries behind them up to
+ * ceil((len_b + n_b) / TADM_PAGE).  At most TADM_STACK_ROWS rows a call; calls on one stack must not overlap.  Rows of a
+ * pooled context are refused (TADM_ERR_STATE): its pool hands out its pages. */
+enum { TADM_STACK_ROWS = 4096 };
+typedef struct {
+  int32_t* id_dev;    /* int32 [size] */
+  int32_t* state_dev; /* int32 [4]: free pages, 0, 0, 0 */
+  int32_t size;
+} tadm_page_stack;
+/* Gives the rows, in their order, the pages that their new tokens need: of all the pages needed, the k-th is the
+ * k-th from the back of the stack.  A row gets all of its pages or none: it is granted if it needs none, or if those needed up
+ * to and with it are no more than the free ones (so that behind a row that had to wait only rows that need none are
+ * granted); one whose positions pass the table is not.  granted_dev [B] receives n_b or 0, a count that
+ * tadm_page_rows takes as n_dev.  slot_dev (int64 [B, n], nullable) receives each granted token's place,
+ * page * TADM_PAGE + position % TADM_PAGE, -1 where there is none or the page is absent.  The entries
+ * of rows that are not granted, and what lies behind the needed ones, stay as they are; the others are written, though
+ * the descriptor's table is const.  Lengths are read on the device, so a captured call serves any; they stay as they are
+ * (the caller advances them). */
+tadm_status tadm_pages_assign(tadm_model* m, const tadm_page_stack* stack, const tadm_page_rows* rows, int32_t n,
+                              int32_t* granted_dev, int64_t* slot_dev);
+/* The reverse: takes back the pages of the rows' last tokens, at positions [len_b, len_b + n_b), len_b being what the row
+ * keeps: the present ones of the entries that these need go onto the stack, rows in their order, entries in theirs,
+ * and the entries become -1.  Pages that several rows name are to come back through one of them. */
+tadm_status tadm_pages_release(tadm_model* m, const tadm_page_stack* stack, const tadm_page_rows* rows, int32_t n);
+
 /* A pool: pages of a model with reference counts, from which contexts take what they need.
  * tadm_pool_create allocates n_pages pages on the model's device (n_pages x n_layers x
  * n_kv_heads x 128 x head_dim bytes).  A pool outlives its contexts (TADM_ERR_STATE

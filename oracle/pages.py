@@ -120,3 +120,41 @@ def attend(q, k, v):
         o[:, h] = (e / total) @ v[h // G]
         lse[h] = (top + np.log(total))[:, 0]
     return o, lse
+
+
+def _up(x):
+    return -(-x // PAGE)
+
+
+def assign(table, lens, news, ids, free, size):
+    """Pages of a stack (ids[:free], taken from the back) for the positions [len, len + new) of the rows of
+    table, in place: (tokens granted to each row, their slots per row, free pages left)."""
+    left, granted, slots = free, [], []
+    waiting = False  # a row that does not get its pages stops those behind it that need some
+    for row, length, new in zip(table, lens, news):
+        if length + new > len(row) * PAGE:
+            new = 0
+        need = range(_up(length), _up(length + new))
+        waiting = waiting or len(need) > left
+        if len(need) and waiting:
+            new, need = 0, ()
+        for e in need:
+            left -= 1
+            row[e] = ids[left]
+        granted.append(new)
+        pages = [row[p // PAGE] for p in range(length, length + new)]
+        slots.append([g * PAGE + p % PAGE if 0 <= g < size else -1 for g, p in zip(pages, range(length, length + new))])
+    return granted, slots, left
+
+
+def release(table, lens, news, ids, free, size):
+    """The pages of the positions [len, len + new) of each row back onto the stack: free pages after it."""
+    for row, length, new in zip(table, lens, news):
+        if length + new > len(row) * PAGE:
+            continue
+        for e in range(_up(length), _up(length + new)):
+            if 0 <= row[e] < size:
+                ids[free] = row[e]
+                free += 1
+            row[e] = -1
+    return free

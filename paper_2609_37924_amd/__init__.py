@@ -65,6 +65,10 @@ class tadm_page_rows(C.Structure):
                 ("max_pages", C.c_int32), ("len", C.c_int32)]
 
 
+class tadm_page_stack(C.Structure):
+    _fields_ = [("id_dev", C.c_void_p), ("state_dev", C.c_void_p), ("size", C.c_int32)]
+
+
 class TadmError(RuntimeError):
     def __init__(self, status, msg):
         super().__init__(f"tadm status {status}: {msg}")
@@ -96,6 +100,8 @@ _SIGS = {
     "tadm_pages_attend_work": (C.c_size_t, [_P, _P, _I]),
     "tadm_pages_read": (_I, [_P, _P, _I, _P, _P, _P, _I]),
     "tadm_pages_copy": (_I, [_P, _P, _P, _P, _I]),
+    "tadm_pages_assign": (_I, [_P, _P, _P, _I, _P, _P]),
+    "tadm_pages_release": (_I, [_P, _P, _P, _I]),
     "tadm_pool_create": (_I, [_P, _I, C.POINTER(_P)]),
     "tadm_pool_destroy": (_I, [_P]),
     "tadm_pool_size": (_I, [_P]),
@@ -137,6 +143,7 @@ for _name, (_res, _args) in _SIGS.items():
 EXPORTED = sorted(_SIGS)
 NOALLOC_MAX_POSITIONS = 65536  # TADM_NOALLOC_MAX_POSITIONS
 PAGE = 64  # TADM_PAGE: positions of a page
+STACK_ROWS = 4096  # TADM_STACK_ROWS: rows of a call on a stack of pages
 
 
 def last_error():
@@ -296,6 +303,27 @@ def tadm_pages_copy(m, pages, src, dst):
     if src.shape != dst.shape or src.ndim != 1:
         raise ValueError(f"{src.shape} sources for {dst.shape} destinations")
     check(lib.tadm_pages_copy(m, C.byref(pages), src.ctypes.data, dst.ctypes.data, len(src)))
+
+
+def page_stack(ids, state):
+    """Descriptor of a stack of free pages: ids int32 [pages in all], the free ones first, state int32 [4] with their
+    number and three zeros, both on the device and kept alive by the caller."""
+    for name, t, ok in (("ids", ids, ids.dim() == 1), ("state", state, tuple(state.shape) == (4,))):
+        if str(t.dtype) != "torch.int32" or not ok or not t.is_contiguous():
+            raise ValueError(f"{name}: {t.dtype} of shape {tuple(t.shape)}, expected contiguous int32")
+    return tadm_page_stack(id_dev=ptr(ids), state_dev=ptr(state), size=ids.shape[0])
+
+
+def tadm_pages_assign(m, stack, rows, n, granted, slots=None):
+    """granted: int32 [B]; slots: optional int64 [B, n]; both contiguous device tensors."""
+    for name, t, kind, shape in (("granted", granted, "torch.int32", (rows.B,)), ("slots", slots, "torch.int64", (rows.B, n))):
+        if t is not None and (str(t.dtype) != kind or tuple(t.shape) != shape or not t.is_contiguous()):
+            raise ValueError(f"{name} must be contiguous {kind} of shape {shape}")
+    check(lib.tadm_pages_assign(m, C.byref(stack), C.byref(rows), n, ptr(granted), ptr(slots)))
+
+
+def tadm_pages_release(m, stack, rows, n):
+    check(lib.tadm_pages_release(m, C.byref(stack), C.byref(rows), n))
 
 
 def tadm_pool_create(m, n_pages):

@@ -36,12 +36,6 @@ struct Args {
   float scale_log2;
 };
 
-__device__ __forceinline__ int row_len(const PageRows& r, int b) {
-  return r.len ? min(max(r.len[b], 0), r.max_len) : r.max_len;
-}
-__device__ __forceinline__ int row_new(const PageRows& r, int b) {
-  return r.n ? min(max(r.n[b], 0), r.max_n) : r.max_n;
-}
 __device__ __forceinline__ float* part_o(const Args& a, size_t col, int split) {
   return a.part + (col * a.S + split) * a.p.dh;
 }

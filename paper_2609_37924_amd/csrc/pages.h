@@ -35,6 +35,12 @@ struct PageRows {
   const int32_t* n;
   int B, max_pages, max_len, max_n;
 };
+__device__ __forceinline__ int row_len(const PageRows& r, int b) {
+  return r.len ? min(max(r.len[b], 0), r.max_len) : r.max_len;
+}
+__device__ __forceinline__ int row_new(const PageRows& r, int b) {
+  return r.n ? min(max(r.n[b], 0), r.max_n) : r.max_n;
+}
 
 // Quantises the window's keys [B, Hkv, cap, dh] and values [B, Hkv, dh, cap] (columns
 // [0, n_b)) into positions [len_b, len_b + n_b) of each row.
@@ -45,6 +51,21 @@ hipError_t pages_read(DType dt, const PageLayer& p, const PageRows& r, void* k, 
 // Page dst[i] <- page src[i], whole pages (src, dst: host arrays, copied into the launch).
 hipError_t pages_copy(void* data, float* scale, size_t page_bytes, size_t page_scales, const int32_t* src,
                       const int32_t* dst, int n, hipStream_t s);
+
+// A stack of free pages in device memory: id[0, free) with free = state[0], the next one taken at the back;
+// size: the pages in all and the entries of id; the other three words of state are 0 outside of a launch.
+struct PageStack {
+  int32_t* id;
+  int32_t* state;
+  int size;
+};
+constexpr int PAGE_STACK_ROWS = 4096;  // rows of a call: the block that takes pages back holds a word of each
+// Pages for the positions [len_b, len_b + n_b) of the rows of `table` (r.table), in the order of the rows; granted [B]
+// tokens that got theirs (n_b or 0), slot (nullable) [B, max_n] their places page * 64 + offset, -1 for the others.
+hipError_t pages_assign(const PageStack& st, const PageRows& r, int32_t* table, int32_t* granted, int64_t* slot,
+                        hipStream_t s);
+// Takes those pages back and clears their entries.
+hipError_t pages_release(const PageStack& st, const PageRows& r, int32_t* table, hipStream_t s);
 
 // table[at[i]] = id[i] (host arrays, copied into the launches).
 hipError_t table_set(int32_t* table, const int32_t* at, const int32_t* id, int n, hipStream_t s);

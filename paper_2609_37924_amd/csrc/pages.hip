@@ -12,12 +12,6 @@
 namespace tadm {
 namespace {
 
-__device__ __forceinline__ int row_len(const PageRows& r, int b) {
-  return r.len ? min(max(r.len[b], 0), r.max_len) : r.max_len;
-}
-__device__ __forceinline__ int row_new(const PageRows& r, int b) {
-  return r.n ? min(max(r.n[b], 0), r.max_n) : r.max_n;
-}
 
 // 2^e of the least e in [PAGE_E_MIN, PAGE_E_MAX] with top <= 448 2^e = 1.75 2^(e + 8)
 __device__ __forceinline__ float scale_of(float top) {

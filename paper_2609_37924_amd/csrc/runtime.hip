@@ -1392,13 +1392,24 @@ static tadm_status check_window_kv(const void* k, const void* vt, int n, int cap
 
 // The rows of a pooled context are read-only: its last page may be others' too, and what is written behind its
 // length raises the scales that its committed positions have.  Only tadm_context_append takes pages for it.
-static tadm_status check_own_table(const tadm_model* m, const tadm_page_rows* r) {
+static tadm_status check_own_table(const tadm_model* m, const tadm_page_rows* r, const char* what) {
   for (const tadm_pool* p : m->page_pools)
     for (const tadm_context* x : p->contexts)
       if (!std::less<const int32_t*>()(r->table_dev, x->table_dev) &&
           std::less<const int32_t*>()(r->table_dev, x->table_dev + x->table.id.size()))
-        return fail(TADM_ERR_STATE, "appending to the rows of a pooled context (tadm_context_append does)");
+        return fail(TADM_ERR_STATE, "%s", what);
   return TADM_OK;
+}
+
+static_assert(PAGE_STACK_ROWS == TADM_STACK_ROWS, "rows of a call on a stack");
+// A stack of free pages and the rows that take from it or give back.
+static tadm_status check_stack(const tadm_page_stack* st, const tadm_page_rows* rows, int n) {
+  if (!st || !st->id_dev || !st->state_dev) return fail(TADM_ERR_INVALID, "null stack of pages");
+  if (st->size < 1) return fail(TADM_ERR_INVALID, "a stack of %d pages", st->size);
+  if (!aligned(st->id_dev, 4) || !aligned(st->state_dev, 4)) return fail(TADM_ERR_INVALID, "stack not aligned to 4 bytes");
+  TRY(check_rows(rows));
+  if (rows->B > TADM_STACK_ROWS) return fail(TADM_ERR_INVALID, "B=%d outside [1, %d]", rows->B, TADM_STACK_ROWS);
+  return check_window_size(rows, n, 0);
 }
 
 static PageLayer page_layer(const tadm_pages* p, int layer) {
@@ -1422,7 +1433,7 @@ tadm_status tadm_pages_append(tadm_model* m, const tadm_pages* p, int32_t layer,
   if (!rows->len_dev && (long)rows->len + n > (long)rows->max_pages * PAGE)
     return fail(TADM_ERR_INVALID, "positions [%d, %ld) with %d pages a row", rows->len, (long)rows->len + n, rows->max_pages);
   TRY(check_page_model(m, p));
-  TRY(check_own_table(m, rows));
+  TRY(check_own_table(m, rows, "appending to the rows of a pooled context (tadm_context_append does)"));
   OnDevice dev(m->device);
   HIPCHK(dev.err);
   HIPCHK(pages_append(m->dt, page_layer(p, layer), page_rows(rows, n), k_dev, vt_dev, cap, m->stream));
@@ -1492,6 +1503,31 @@ tadm_status tadm_pages_copy(tadm_model* m, const tadm_pages* p, const int32_t* s
   HIPCHK(dev.err);
   const PageLayer pl = page_layer(p, 0);
   HIPCHK(pages_copy(p->data, p->scale, pl.page_bytes, pl.page_scales, src, dst, n_copies, m->stream));
+  return TADM_OK;
+}
+
+tadm_status tadm_pages_assign(tadm_model* m, const tadm_page_stack* stack, const tadm_page_rows* rows, int32_t n,
+                              int32_t* granted_dev, int64_t* slot_dev) {
+  TRY(check_stack(stack, rows, n));
+  if (!granted_dev) return fail(TADM_ERR_INVALID, "null granted_dev");
+  if (!aligned(granted_dev, 4) || !aligned(slot_dev, 8)) return fail(TADM_ERR_INVALID, "granted_dev or slot_dev not aligned");
+  if (!m) return fail(TADM_ERR_INVALID, "null model");
+  TRY(check_own_table(m, rows, "pages for the rows of a pooled context (tadm_context_append takes them)"));
+  OnDevice dev(m->device);
+  HIPCHK(dev.err);
+  HIPCHK(pages_assign(PageStack{stack->id_dev, stack->state_dev, stack->size}, page_rows(rows, n),
+                      const_cast<int32_t*>(rows->table_dev), granted_dev, slot_dev, m->stream));
+  return TADM_OK;
+}
+
+tadm_status tadm_pages_release(tadm_model* m, const tadm_page_stack* stack, const tadm_page_rows* rows, int32_t n) {
+  TRY(check_stack(stack, rows, n));
+  if (!m) return fail(TADM_ERR_INVALID, "null model");
+  TRY(check_own_table(m, rows, "pages of a pooled context (tadm_context_truncate gives them back)"));
+  OnDevice dev(m->device);
+  HIPCHK(dev.err);
+  HIPCHK(pages_release(PageStack{stack->id_dev, stack->state_dev, stack->size}, page_rows(rows, n),
+                       const_cast<int32_t*>(rows->table_dev), m->stream));
   return TADM_OK;
 }
 
