@@ -388,6 +388,32 @@ tadm_status tadm_sample_noalloc(tadm_model* m, const float* logits_dev, const in
                                 const tadm_step_args* args, int32_t* next_canvas_dev,
                                 int32_t* choice_dev, float* conf_dev);
 
+/* One token of each row of logits [R, vocab] (rows ld floats apart, at any float; vocab the model's) from a given
+ * uniform number, each row with settings of its own: device arrays [R], a NULL one leaving its setting off.
+ *   l' = l (1 / temperature); q_v = rint(exp(l'_v - max l') 2^40), with the float32 exponential of tadm_sample: whole
+ *   numbers, so that a draw is the same wherever and however it is summed; NaN and -inf weigh nothing.
+ *   The entries are ordered by l' descending, ties by the lowest id, and kept are
+ *     of all, the first top_k (top_k < 1 or >= vocab: all), weighing Q;
+ *     of these, the shortest prefix that weighs ceil(ceil(2^24 top_p) Q / 2^24) or more (top_p >= 1: all; at least the first);
+ *     of these, those with q >= ceil(2^40 min_p), weighing T (the first has q = 2^40 and stays).
+ *   token_dev[r]: the lowest id at which the running sum of the kept q in the order of the ids exceeds
+ *     floor(floor(2^24 u) T / 2^24), u_dev[r] in [0, 1) (values outside are cut to it);
+ *   logp_dev[r] (nullable): log(q / T) of that token.
+ * A temperature of 0 or less takes the first entry of the order, with logp 0.  Entries of +inf are a maximum like any
+ * other.  A row of NaN and -inf alone gets -1 and -inf.  work_dev (16-byte aligned, NULL when the size is 0) is scratch of at
+ * least tadm_sample_rows_work bytes; calls that may overlap, captured ones among them, need scratch of their own. */
+enum { TADM_SAMPLE_ROWS = 1 << 21 }; /* rows of a call at most */
+typedef struct {
+  const float* temperature_dev;
+  const int32_t* top_k_dev;
+  const float* top_p_dev;
+  const float* min_p_dev;
+} tadm_row_settings;
+tadm_status tadm_sample_rows(tadm_model* m, const float* logits_dev, int64_t ld, int32_t R, const tadm_row_settings* set,
+                             const float* u_dev, int32_t* token_dev, float* logp_dev, void* work_dev, size_t work_bytes);
+/* Scratch of a tadm_sample_rows call of R rows; 0 for invalid arguments. */
+size_t tadm_sample_rows_work(const tadm_model* m, int32_t R);
+
 /* Whole generation (Algorithm 1 with the linear unmask schedule
  * n_i = floor(M0 i / T) - floor(M0 (i-1) / T)).  prompt_dev [B, P]; tokens_dev
  * [B, P + gen_len] receives prompt and generated tokens.  block_len == gen_len:

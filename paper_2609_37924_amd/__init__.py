@@ -69,6 +69,11 @@ class tadm_page_stack(C.Structure):
     _fields_ = [("id_dev", C.c_void_p), ("state_dev", C.c_void_p), ("size", C.c_int32)]
 
 
+class tadm_row_settings(C.Structure):
+    _fields_ = [("temperature_dev", C.c_void_p), ("top_k_dev", C.c_void_p), ("top_p_dev", C.c_void_p),
+                ("min_p_dev", C.c_void_p)]
+
+
 class TadmError(RuntimeError):
     def __init__(self, status, msg):
         super().__init__(f"tadm status {status}: {msg}")
@@ -119,6 +124,8 @@ _SIGS = {
     "tadm_denoise_step": (_I, [_P, _P, _P, _I, _I, _I, _P, C.POINTER(tadm_step_args), _P, _P]),
     "tadm_sample": (_I, [_P, _P, _P, _I, _I, _I, _I, C.POINTER(tadm_step_args), _P, _P, _P]),
     "tadm_sample_noalloc": (_I, [_P, _P, _P, _I, _I, _I, _I, C.POINTER(tadm_step_args), _P, _P, _P]),
+    "tadm_sample_rows": (_I, [_P, _P, C.c_int64, _I, _P, _P, _P, _P, _P, C.c_size_t]),
+    "tadm_sample_rows_work": (C.c_size_t, [_P, _I]),
     "tadm_generate": (_I, [_P, _P, _I, _I, _I, _I, _I, _I, C.c_uint64, C.c_float, _P]),
     "tadm_generate_sampler": (_I, [_P, _P, _I, _I, _I, _I, _I, _I, C.c_uint64, C.c_float,
                                    C.POINTER(tadm_sampler), _P]),
@@ -438,6 +445,39 @@ def tadm_sample(m, logits, canvas, B, L, canvas_off, pos0, args, next_canvas, ch
 def tadm_sample_noalloc(m, logits, canvas, B, L, canvas_off, pos0, args, next_canvas, choice=None, conf=None):
     check(lib.tadm_sample_noalloc(m, ptr(logits), ptr(canvas), B, L, canvas_off, pos0, C.byref(args),
                                   ptr(next_canvas), ptr(choice), ptr(conf)))
+
+
+def row_settings(temperature=None, top_k=None, top_p=None, min_p=None):
+    """Settings of each row of a tadm_sample_rows call: contiguous device tensors [R] (float32, top_k int32), None for
+    a setting that is off.  The caller keeps the tensors alive."""
+    given = dict(temperature=temperature, top_k=top_k, top_p=top_p, min_p=min_p)
+    for name, t in given.items():
+        kind = "torch.int32" if name == "top_k" else "torch.float32"
+        if t is not None and (str(t.dtype) != kind or t.dim() != 1 or not t.is_contiguous()):
+            raise ValueError(f"{name} must be contiguous {kind} with an entry for each row")
+    s = tadm_row_settings(**{name + "_dev": ptr(t) for name, t in given.items()})
+    s.rows = {t.shape[0] for t in given.values() if t is not None}
+    return s
+
+
+def tadm_sample_rows(m, logits, settings, u, token, logp=None, work=None):
+    """logits: float32 [R, vocab], rows at any stride; settings: row_settings or None; u, logp: float32 [R];
+    token: int32 [R]; work: a device tensor of at least tadm_sample_rows_work bytes (None when that is 0)."""
+    if str(logits.dtype) != "torch.float32" or logits.dim() != 2 or logits.stride(1) != 1:
+        raise ValueError(f"logits: {logits.dtype} of shape {tuple(logits.shape)}, expected float32 rows")
+    R = logits.shape[0]
+    for name, t, kind in (("u", u, "torch.float32"), ("token", token, "torch.int32"), ("logp", logp, "torch.float32")):
+        if t is not None and (str(t.dtype) != kind or tuple(t.shape) != (R,) or not t.is_contiguous()):
+            raise ValueError(f"{name} must be contiguous {kind} of {R} rows")
+    if settings is not None and settings.rows - {R}:
+        raise ValueError(f"settings of {settings.rows} rows for {R}")
+    check(lib.tadm_sample_rows(m, ptr(logits), logits.stride(0) if R > 1 else max(logits.stride(0), logits.shape[1]), R,
+                               None if settings is None else C.byref(settings), ptr(u), ptr(token), ptr(logp), ptr(work),
+                               0 if work is None else work.numel() * work.element_size()))
+
+
+def tadm_sample_rows_work(m, R):
+    return lib.tadm_sample_rows_work(m, R)
 
 
 def tadm_generate(m, prompt, B, P, gen_len, T, K, block_len, seed, temperature, tokens):

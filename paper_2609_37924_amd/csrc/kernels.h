@@ -279,6 +279,20 @@ hipError_t nucleus_thresholds(const float* logits, const int32_t* row_map, const
 hipError_t sample_tokens(const float* logits, const int32_t* row_map, const NucleusThr* thr, const int32_t* canvas,
                          int B, int L, int canvas_off, int V, int mask_id, int pos0, uint32_t step_id,
                          uint64_t seed, float inv_temp, int32_t* choice, float* conf, hipStream_t s);
+// One token of each of R rows of V logits, ld apart, from u[r] in [0, 1) and the row's settings (each array
+// nullable: 1, 0, 1 and 0), and its log-probability in what these leave (draw.hip).
+constexpr int DRAW_MAX_VOCAB = 1024 * 256;
+struct DrawRows {
+  const float* logits;
+  size_t ld;
+  int R, V;
+  const float* temperature;
+  const int32_t* top_k;
+  const float *top_p, *min_p, *u;
+  int32_t* token;
+  float* logp;  // nullable
+};
+hipError_t draw_rows(const DrawRows& d, hipStream_t s);
 // Per row: reveal the n most confident masked positions (n = n_rows[b] if n_rows is
 // set, else n_unmask; clamped to the row's masked count); copy the rest.
 hipError_t select_unmask(const int32_t* canvas, const int32_t* choice, const float* conf, int B,

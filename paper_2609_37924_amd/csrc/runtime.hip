@@ -2022,6 +2022,32 @@ tadm_status tadm_sample_noalloc(tadm_model* m, const float* logits_dev, const in
   return TADM_OK;
 }
 
+size_t tadm_sample_rows_work(const tadm_model* m, int32_t R) {
+  return 0;
+}
+
+tadm_status tadm_sample_rows(tadm_model* m, const float* logits_dev, int64_t ld, int32_t R, const tadm_row_settings* set,
+                             const float* u_dev, int32_t* token_dev, float* logp_dev, void* work_dev,
+                             size_t work_bytes) {
+  if (!logits_dev || !u_dev || !token_dev) return fail(TADM_ERR_INVALID, "null logits, u_dev or token_dev");
+  if (R < 1 || R > TADM_SAMPLE_ROWS) return fail(TADM_ERR_INVALID, "R=%d outside [1, %d]", R, TADM_SAMPLE_ROWS);
+  const tadm_row_settings none{}, &a = set ? *set : none;
+  for (const void* p : {(const void*)logits_dev, (const void*)u_dev, (const void*)token_dev, (const void*)logp_dev,
+                        (const void*)a.temperature_dev, (const void*)a.top_k_dev, (const void*)a.top_p_dev,
+                        (const void*)a.min_p_dev})
+    if (!aligned(p, 4)) return fail(TADM_ERR_INVALID, "array not aligned to 4 bytes");
+  if (!m) return fail(TADM_ERR_INVALID, "null model");
+  if (ld < m->cfg.vocab) return fail(TADM_ERR_INVALID, "rows of %d logits %lld apart", m->cfg.vocab, (long long)ld);
+  const size_t need = tadm_sample_rows_work(m, R);
+  if (need && (!work_dev || work_bytes < need || !aligned(work_dev, 16)))
+    return fail(TADM_ERR_INVALID, "scratch of %zu bytes, %zu needed, aligned to 16", work_dev ? work_bytes : 0, need);
+  OnDevice dev(m->device);
+  HIPCHK(dev.err);
+  HIPCHK(draw_rows(DrawRows{logits_dev, (size_t)ld, R, m->cfg.vocab, a.temperature_dev, a.top_k_dev, a.top_p_dev,
+                            a.min_p_dev, u_dev, token_dev, logp_dev}, m->stream));
+  return TADM_OK;
+}
+
 // --------------------------------------------------------------- generate ---
 // Algorithm 1 per block; the model-owned cache, context and window are reused
 // across calls, so a warm generation allocates nothing and never synchronises.
