@@ -237,6 +237,33 @@ tadm_status tadm_pages_attend(tadm_model* m, const tadm_pages* p, int32_t layer,
                               void* o_dev, float* lse_dev, void* work_dev, size_t work_bytes);
 /* Scratch of a tadm_pages_attend call with these rows (B and len) and n; 0 for invalid arguments. */
 size_t tadm_pages_attend_work(const tadm_model* m, const tadm_page_rows* rows, int32_t n);
+/* Attention for rows that share their leading pages, as the samples of one prompt do: the shared pages are read
+ * once for all of them.  tadm_pages_share finds the groups, runs of rows that have at least min_pages (>= 1) whole
+ * leading pages in common with the row before (equal table entries within both rows' lengths; what a group shares
+ * is what all of its rows have in common), and lays out in plan->data_dev the work of the calls that follow, for
+ * windows of n tokens: a pass calls it once, before its layers.  lead_dev and pages_dev ([B], nullable) receive each
+ * row's group by its first row and the pages that the group shares (0 in a group of one).  data_dev is 16-byte aligned and
+ * holds tadm_pages_plan_bytes; the other fields are set by the call.  A plan is of the tables and lengths as they are when it
+ * runs: after a change of either it is to be made again (its values are void then, no access leaves the arrays).
+ * At most TADM_SHARE_ROWS rows. */
+enum { TADM_SHARE_ROWS = 1024 };
+typedef struct {
+  int32_t* data_dev;
+  size_t bytes;
+  int32_t B, max_pages, len, n, n_heads, n_kv_heads, dtype;
+} tadm_page_plan;
+tadm_status tadm_pages_share(tadm_model* m, const tadm_page_rows* rows, int32_t n, int32_t min_pages,
+                             tadm_page_plan* plan, int32_t* lead_dev, int32_t* pages_dev);
+/* Bytes of a plan of these rows (B) and n; 0 for invalid arguments. */
+size_t tadm_pages_plan_bytes(const tadm_model* m, const tadm_page_rows* rows, int32_t n);
+/* tadm_pages_attend, with the same arguments and results (sums in another order), as the plan says.  TADM_ERR_STATE for
+ * a plan of other rows, another n or other heads.  The scratch, of at least tadm_pages_attend_shared_work bytes, is for one call
+ * at a time, as there; a plan may serve calls that overlap. */
+tadm_status tadm_pages_attend_shared(tadm_model* m, const tadm_pages* p, int32_t layer, const tadm_page_rows* rows,
+                                     const tadm_page_plan* plan, const void* q_dev, int32_t n, const void* k_dev,
+                                     const void* vt_dev, int32_t cap, void* o_dev, float* lse_dev, void* work_dev,
+                                     size_t work_bytes);
+size_t tadm_pages_attend_shared_work(const tadm_model* m, const tadm_page_rows* rows, int32_t n);
 /* The positions [0, len_b) of one layer as keys k_dev [B, Hkv, cap, head_dim] and transposed
  * values vt_dev [B, Hkv, head_dim, cap] of the model dtype, exactly; zeros for absent
  * pages, other columns stay as they are.  cap >= len, a multiple of 64. */
@@ -318,6 +345,11 @@ tadm_status tadm_context_fork(const tadm_context* src, const int32_t* rows, int3
  * stay as the dropped positions left them: where those had raised the scale, the ones that remain
  * are rounded to it, and so are those appended next.  At whole pages nothing is left of what was dropped. */
 tadm_status tadm_context_truncate(tadm_context* ctx, int32_t len);
+/* Passes over a pooled context read what neighbouring rows share (the rows of a fork that come from one row) once
+ * for all of them, from min_pages (>= 1) shared pages on; 0: each row by itself, as after creation and in a fork.  The
+ * results are the same up to the order of sums.  Allocates scratch; not under graph capture (TADM_ERR_STATE), and
+ * passes captured before keep what they were captured with.  TADM_ERR_UNSUPPORTED for more than TADM_SHARE_ROWS rows. */
+tadm_status tadm_context_share(tadm_context* ctx, int32_t min_pages);
 /* The rows of a pooled context for the operators above (valid until it is destroyed; len as of now).
  * Behind the context's pages the table has absent ones. */
 tadm_status tadm_context_rows(const tadm_context* ctx, tadm_page_rows* out);

@@ -158,3 +158,19 @@ def release(table, lens, news, ids, free, size):
                 free += 1
             row[e] = -1
     return free
+
+
+def groups(table, lens, min_pages=1):
+    """(first row of each row's group, pages that the group shares): neighbours with min_pages or more whole
+    leading pages in common stand in one group, which shares what all of them do; 0 for a row alone."""
+    lead, shared = [], [0] * len(table)
+    for b, row in enumerate(table):
+        common = 0
+        while b and common < min(lens[b], lens[b - 1]) // PAGE and row[common] == table[b - 1][common]:
+            common += 1
+        if b and common >= min_pages:
+            lead.append(lead[-1])
+            shared[lead[b]] = min(shared[lead[b]], common) if shared[lead[b]] else common
+        else:
+            lead.append(b)
+    return lead, [shared[a] for a in lead]

@@ -65,6 +65,11 @@ class tadm_page_rows(C.Structure):
                 ("max_pages", C.c_int32), ("len", C.c_int32)]
 
 
+class tadm_page_plan(C.Structure):
+    _fields_ = [("data_dev", C.c_void_p), ("bytes", C.c_size_t)] + [
+        (n, C.c_int32) for n in ("B", "max_pages", "len", "n", "n_heads", "n_kv_heads", "dtype")]
+
+
 class tadm_page_stack(C.Structure):
     _fields_ = [("id_dev", C.c_void_p), ("state_dev", C.c_void_p), ("size", C.c_int32)]
 
@@ -105,6 +110,10 @@ _SIGS = {
     "tadm_pages_attend_work": (C.c_size_t, [_P, _P, _I]),
     "tadm_pages_read": (_I, [_P, _P, _I, _P, _P, _P, _I]),
     "tadm_pages_copy": (_I, [_P, _P, _P, _P, _I]),
+    "tadm_pages_share": (_I, [_P, _P, _I, _I, _P, _P, _P]),
+    "tadm_pages_plan_bytes": (C.c_size_t, [_P, _P, _I]),
+    "tadm_pages_attend_shared": (_I, [_P, _P, _I, _P, _P, _P, _I, _P, _P, _I, _P, _P, _P, C.c_size_t]),
+    "tadm_pages_attend_shared_work": (C.c_size_t, [_P, _P, _I]),
     "tadm_pages_assign": (_I, [_P, _P, _P, _I, _P, _P]),
     "tadm_pages_release": (_I, [_P, _P, _P, _I]),
     "tadm_pool_create": (_I, [_P, _I, C.POINTER(_P)]),
@@ -117,6 +126,7 @@ _SIGS = {
     "tadm_context_create_pooled": (_I, [_P, _P, _I, _I, C.POINTER(_P)]),
     "tadm_context_fork": (_I, [_P, _P, _I, C.POINTER(_P)]),
     "tadm_context_truncate": (_I, [_P, _I]),
+    "tadm_context_share": (_I, [_P, _I]),
     "tadm_context_rows": (_I, [_P, C.POINTER(tadm_page_rows)]),
     "tadm_entropy_inv_temp": (C.c_float, [_I, _I, C.c_float, C.c_float]),
     "tadm_train_loss": (_I, [_P, _P, _I, _I, _P, _P, C.c_float, C.c_uint64, C.c_uint32, _P, _P, _P, _P]),
@@ -150,6 +160,7 @@ for _name, (_res, _args) in _SIGS.items():
 EXPORTED = sorted(_SIGS)
 NOALLOC_MAX_POSITIONS = 65536  # TADM_NOALLOC_MAX_POSITIONS
 PAGE = 64  # TADM_PAGE: positions of a page
+SHARE_ROWS = 1024  # TADM_SHARE_ROWS: rows of a plan
 STACK_ROWS = 4096  # TADM_STACK_ROWS: rows of a call on a stack of pages
 
 
@@ -299,6 +310,37 @@ def tadm_pages_attend_work(m, rows, n):
     return lib.tadm_pages_attend_work(m, C.byref(rows), n)
 
 
+def page_plan(data):
+    """Descriptor of a plan that tadm_pages_share lays out in a device tensor of at least tadm_pages_plan_bytes,
+    kept alive by the caller."""
+    if not data.is_contiguous():
+        raise ValueError("a plan must be contiguous")
+    return tadm_page_plan(data_dev=ptr(data), bytes=data.numel() * data.element_size())
+
+
+def tadm_pages_plan_bytes(m, rows, n):
+    return lib.tadm_pages_plan_bytes(m, C.byref(rows), n)
+
+
+def tadm_pages_share(m, rows, n, min_pages, plan, lead=None, pages=None):
+    """lead, pages: optional contiguous int32 [B] device tensors."""
+    for name, t in (("lead", lead), ("pages", pages)):
+        if t is not None and (str(t.dtype) != "torch.int32" or tuple(t.shape) != (rows.B,) or not t.is_contiguous()):
+            raise ValueError(f"{name} must be contiguous int32 of {rows.B} rows")
+    check(lib.tadm_pages_share(m, C.byref(rows), n, min_pages, C.byref(plan), ptr(lead), ptr(pages)))
+
+
+def tadm_pages_attend_shared(m, pages, layer, rows, plan, q, n, k, vt, cap, o, lse, work):
+    """work: a device tensor of at least tadm_pages_attend_shared_work bytes."""
+    check(lib.tadm_pages_attend_shared(m, C.byref(pages), layer, C.byref(rows), C.byref(plan), ptr(q), n, ptr(k), ptr(vt),
+                                       cap, ptr(o), ptr(lse), ptr(work),
+                                       0 if work is None else work.numel() * work.element_size()))
+
+
+def tadm_pages_attend_shared_work(m, rows, n):
+    return lib.tadm_pages_attend_shared_work(m, C.byref(rows), n)
+
+
 def tadm_pages_read(m, pages, layer, rows, k, vt, cap):
     check(lib.tadm_pages_read(m, C.byref(pages), layer, C.byref(rows), ptr(k), ptr(vt), cap))
 
@@ -380,6 +422,10 @@ def tadm_context_fork(src, rows):
 
 def tadm_context_truncate(ctx, length):
     check(lib.tadm_context_truncate(ctx, length))
+
+
+def tadm_context_share(ctx, min_pages):
+    check(lib.tadm_context_share(ctx, min_pages))
 
 
 def tadm_context_rows(ctx):

@@ -90,4 +90,17 @@ size_t page_attend_work(DType dt, int B, int H, int Hkv, int dh, int L, int max_
 size_t page_attend_threads(DType dt, int B, int H, int Hkv, int dh, int L, int max_len);
 hipError_t page_attend(DType dt, const PageAttend& a, hipStream_t s);
 
+// The same for rows of which neighbours may share their leading pages (page_shared.hip): those are read once for all
+// that share them.  page_plan finds the groups, runs of rows that have min_pages whole leading pages or more in
+// common with the row before, and lays out what the blocks of page_attend_shared do with these rows' tables and
+// lengths (plan: page_plan_bytes(), 16-byte aligned); lead, pages (nullable, [B]): each row's group by its first row, and the
+// pages that the group has in common.
+constexpr int PAGE_SHARE_ROWS = 1024;  // rows of a plan: a thread of a block each
+size_t page_plan_bytes(DType dt, int B, int H, int Hkv, int L);
+size_t page_shared_work(DType dt, int B, int H, int Hkv, int dh, int L);
+size_t page_shared_threads(DType dt, int B, int H, int Hkv, int L);
+hipError_t page_plan(DType dt, const PageRows& r, int H, int Hkv, int min_pages, int32_t* plan, int32_t* lead,
+                     int32_t* pages, hipStream_t s);
+hipError_t page_attend_shared(DType dt, const PageAttend& a, const int32_t* plan, hipStream_t s);
+
 }  // namespace tadm

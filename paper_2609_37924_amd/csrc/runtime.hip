@@ -342,6 +342,11 @@ struct tadm_context {
   void* work = nullptr;  // scratch of the attention: the most that any window needs
   size_t work_bytes = 0;
   bool appending = false;  // the running pass commits its K, V
+  // rows that share this many pages or more are attended to together (0: each row by itself), with a plan that
+  // each part of a pass makes and scratch of its own
+  int share = 0;
+  int32_t* plan = nullptr;
+  void* share_work = nullptr;
 };
 
 // ---------------------------------------------------------------- profiling ---
@@ -556,7 +561,11 @@ static tadm_status run_layer(tadm_model* m, int li, float* x, int B, int L, int 
   if (kv.pages) {
     const PageLayer pl = pool_layer(kv.pages->pool, li);
     const PageRows rows = context_rows(kv.pages, L);
-    HIPCHK(page_attend(m->dt, PageAttend{pl, rows, s.q, kv.k, kv.vt, s.ao, nullptr, H, kv.cap, kv.pages->work}, st));
+    if (kv.pages->share)
+      HIPCHK(page_attend_shared(m->dt, PageAttend{pl, rows, s.q, kv.k, kv.vt, s.ao, nullptr, H, kv.cap, kv.pages->share_work},
+                                kv.pages->plan, st));
+    else
+      HIPCHK(page_attend(m->dt, PageAttend{pl, rows, s.q, kv.k, kv.vt, s.ao, nullptr, H, kv.cap, kv.pages->work}, st));
     if (kv.pages->appending) HIPCHK(pages_append(m->dt, pl, rows, kv.k, kv.vt, kv.cap, st));
   } else {
     HIPCHK(attention(m->dt, s.q, kv.k, kv.vt, s.ao, B, H, Hk, L, kv.off + L, kv.cap, dh, st));
@@ -642,6 +651,9 @@ static KVTarget kv_target(tadm_model* m, const tadm_context* ctx, int li) {
 static tadm_status run_part(tadm_model* m, int first, int count, float* x, int B, int L, int pos0,
                             const tadm_context* ctx, bool prenormed = false) {
   bool pre = prenormed;
+  if (count > 0 && ctx && ctx->pool && ctx->share)
+    HIPCHK(page_plan(m->dt, context_rows(ctx, L), m->cfg.n_heads, m->cfg.n_kv_heads, ctx->share, ctx->plan, nullptr, nullptr,
+                     m->stream));
   for (int li = first; li < first + count; ++li) {
     const float* next_norm = li + 1 < first + count ? m->Wf(m->lay.layers[li + 1].attn_norm) : nullptr;
     bool next_pre = false;
@@ -1323,7 +1335,8 @@ tadm_status tadm_context_destroy(tadm_context* ctx) {
     all.erase(std::remove(all.begin(), all.end(), ctx), all.end());
   }
   if (ctx->table_dev) (void)hipFree(ctx->table_dev);
-  if (ctx->work) (void)hipFree(ctx->work);
+  for (void* p : {ctx->work, (void*)ctx->plan, ctx->share_work})
+    if (p) (void)hipFree(p);
   delete ctx;
   return TADM_OK;
 }
@@ -1401,6 +1414,7 @@ static tadm_status check_own_table(const tadm_model* m, const tadm_page_rows* r,
   return TADM_OK;
 }
 
+static_assert(PAGE_SHARE_ROWS == TADM_SHARE_ROWS, "rows of a plan");
 static_assert(PAGE_STACK_ROWS == TADM_STACK_ROWS, "rows of a call on a stack");
 // A stack of free pages and the rows that take from it or give back.
 static tadm_status check_stack(const tadm_page_stack* st, const tadm_page_rows* rows, int n) {
@@ -1464,6 +1478,77 @@ tadm_status tadm_pages_attend(tadm_model* m, const tadm_pages* p, int32_t layer,
   HIPCHK(dev.err);
   HIPCHK(page_attend(m->dt, PageAttend{page_layer(p, layer), page_rows(rows, n), q_dev, k_dev, vt_dev, o_dev, lse_dev,
                                        m->cfg.n_heads, cap, work_dev}, m->stream));
+  return TADM_OK;
+}
+
+// Rows, a window and the model's heads within what a plan and its calls take.
+static tadm_status check_share_size(const tadm_model* m, const tadm_page_rows* rows, int n) {
+  TRY(check_rows(rows));
+  if (rows->B > TADM_SHARE_ROWS) return fail(TADM_ERR_INVALID, "B=%d outside [1, %d]", rows->B, TADM_SHARE_ROWS);
+  TRY(check_window_size(rows, n, 0));
+  if (!m) return fail(TADM_ERR_INVALID, "null model");
+  const tadm_config& c = m->cfg;
+  TRY(check_window_size(rows, n, c.n_heads));
+  if (page_shared_threads(m->dt, rows->B, c.n_heads, c.n_kv_heads, n) >> 32)
+    return fail(TADM_ERR_INVALID, "%d rows of %d K/V heads: too many in one call, whose launch takes 2^32 threads", rows->B,
+                c.n_kv_heads);
+  return TADM_OK;
+}
+
+size_t tadm_pages_plan_bytes(const tadm_model* m, const tadm_page_rows* rows, int32_t n) {
+  if (check_share_size(m, rows, n) != TADM_OK) return 0;
+  return page_plan_bytes(m->dt, rows->B, m->cfg.n_heads, m->cfg.n_kv_heads, n);
+}
+
+size_t tadm_pages_attend_shared_work(const tadm_model* m, const tadm_page_rows* rows, int32_t n) {
+  if (check_share_size(m, rows, n) != TADM_OK) return 0;
+  return page_shared_work(m->dt, rows->B, m->cfg.n_heads, m->cfg.n_kv_heads, m->cfg.head_dim, n);
+}
+
+tadm_status tadm_pages_share(tadm_model* m, const tadm_page_rows* rows, int32_t n, int32_t min_pages,
+                             tadm_page_plan* plan, int32_t* lead_dev, int32_t* pages_dev) {
+  TRY(check_rows(rows));
+  if (!plan || !plan->data_dev || !aligned(plan->data_dev, 16)) return fail(TADM_ERR_INVALID, "null plan, or not aligned to 16 bytes");
+  if (min_pages < 1) return fail(TADM_ERR_INVALID, "min_pages=%d", min_pages);
+  if (!aligned(lead_dev, 4) || !aligned(pages_dev, 4)) return fail(TADM_ERR_INVALID, "lead_dev or pages_dev not aligned to 4 bytes");
+  TRY(check_share_size(m, rows, n));
+  const size_t need = tadm_pages_plan_bytes(m, rows, n);
+  if (plan->bytes < need) return fail(TADM_ERR_INVALID, "plan of %zu bytes, %zu needed", plan->bytes, need);
+  OnDevice dev(m->device);
+  HIPCHK(dev.err);
+  const tadm_config& c = m->cfg;
+  HIPCHK(page_plan(m->dt, page_rows(rows, n), c.n_heads, c.n_kv_heads, min_pages, plan->data_dev, lead_dev, pages_dev,
+                   m->stream));
+  *plan = tadm_page_plan{plan->data_dev, plan->bytes, rows->B, rows->max_pages, rows->len, n, c.n_heads, c.n_kv_heads, c.dtype};
+  return TADM_OK;
+}
+
+tadm_status tadm_pages_attend_shared(tadm_model* m, const tadm_pages* p, int32_t layer, const tadm_page_rows* rows,
+                                     const tadm_page_plan* plan, const void* q_dev, int32_t n, const void* k_dev,
+                                     const void* vt_dev, int32_t cap, void* o_dev, float* lse_dev, void* work_dev,
+                                     size_t work_bytes) {
+  TRY(check_pages(p, layer));
+  TRY(check_rows(rows));
+  TRY(check_window_size(rows, n, 0));
+  if (!plan || !plan->data_dev) return fail(TADM_ERR_INVALID, "null plan");
+  if (!q_dev || !o_dev) return fail(TADM_ERR_INVALID, "null queries or output");
+  if (!aligned(q_dev, 16) || !aligned(o_dev, 16) || !aligned(lse_dev, 4))
+    return fail(TADM_ERR_INVALID, "queries or output not aligned to 16 bytes");
+  if (k_dev || vt_dev) TRY(check_window_kv(k_dev, vt_dev, n, cap));
+  TRY(check_page_model(m, p));
+  TRY(check_share_size(m, rows, n));
+  const tadm_config& c = m->cfg;
+  if (plan->B != rows->B || plan->max_pages != rows->max_pages || plan->len != rows->len || plan->n != n ||
+      plan->n_heads != c.n_heads || plan->n_kv_heads != c.n_kv_heads || plan->dtype != c.dtype)
+    return fail(TADM_ERR_STATE, "plan of %d rows of up to %d positions and %d tokens, %d heads over %d", plan->B, plan->len,
+                plan->n, plan->n_heads, plan->n_kv_heads);
+  const size_t need = tadm_pages_attend_shared_work(m, rows, n);
+  if (!work_dev || work_bytes < need || !aligned(work_dev, 16))
+    return fail(TADM_ERR_INVALID, "scratch of %zu bytes, %zu needed, aligned to 16", work_dev ? work_bytes : 0, need);
+  OnDevice dev(m->device);
+  HIPCHK(dev.err);
+  HIPCHK(page_attend_shared(m->dt, PageAttend{page_layer(p, layer), page_rows(rows, n), q_dev, k_dev, vt_dev, o_dev, lse_dev,
+                                              c.n_heads, cap, work_dev}, plan->data_dev, m->stream));
   return TADM_OK;
 }
 
@@ -1725,6 +1810,38 @@ tadm_status tadm_context_fork(const tadm_context* src, const int32_t* rows, int3
     return fail(TADM_ERR_DEVICE, "fork: %s", hipGetErrorString(e));
   }
   *out = x;
+  return TADM_OK;
+}
+
+tadm_status tadm_context_share(tadm_context* ctx, int32_t min_pages) {
+  if (!ctx) return fail(TADM_ERR_INVALID, "null context");
+  if (min_pages < 0) return fail(TADM_ERR_INVALID, "min_pages=%d", min_pages);
+  if (!ctx->pool) return fail(TADM_ERR_STATE, "the context has no pages");
+  tadm_model* m = ctx->model;
+  TRY(check_no_capture(m, "tadm_context_share"));
+  if (min_pages && ctx->B > TADM_SHARE_ROWS)
+    return fail(TADM_ERR_UNSUPPORTED, "B=%d rows, at most %d share pages", ctx->B, TADM_SHARE_ROWS);
+  if (min_pages && !ctx->plan) {
+    OnDevice dev(m->device);
+    HIPCHK(dev.err);
+    const tadm_config& c = m->cfg;
+    size_t work = 0, plan = 0;
+    for (int n = 1; n <= c.max_seq; ++n) {
+      work = std::max(work, page_shared_work(m->dt, ctx->B, c.n_heads, c.n_kv_heads, c.head_dim, n));
+      plan = std::max(plan, page_plan_bytes(m->dt, ctx->B, c.n_heads, c.n_kv_heads, n));
+    }
+    void *w = nullptr, *p = nullptr;
+    hipError_t e = hipMalloc(&w, work);
+    if (e == hipSuccess) e = hipMalloc(&p, plan);
+    if (e != hipSuccess) {
+      if (w) (void)hipFree(w);
+      return fail(e == hipErrorOutOfMemory ? TADM_ERR_OOM : TADM_ERR_DEVICE, "sharing (%zu bytes): %s", work + plan,
+                  hipGetErrorString(e));
+    }
+    ctx->share_work = w;
+    ctx->plan = static_cast<int32_t*>(p);
+  }
+  ctx->share = min_pages;
   return TADM_OK;
 }
 
