@@ -292,7 +292,8 @@ struct DrawRows {
   int32_t* token;
   float* logp;  // nullable
 };
-hipError_t draw_rows(const DrawRows& d, hipStream_t s);
+size_t draw_work(int R, int V);  // scratch (16-byte aligned) of such a call
+hipError_t draw_rows(const DrawRows& d, void* work, hipStream_t s);
 // Per row: reveal the n most confident masked positions (n = n_rows[b] if n_rows is
 // set, else n_unmask; clamped to the row's masked count); copy the rest.
 hipError_t select_unmask(const int32_t* canvas, const int32_t* choice, const float* conf, int B,

@@ -2140,7 +2140,7 @@ tadm_status tadm_sample_noalloc(tadm_model* m, const float* logits_dev, const in
 }
 
 size_t tadm_sample_rows_work(const tadm_model* m, int32_t R) {
-  return 0;
+  return m && R >= 1 && R <= TADM_SAMPLE_ROWS ? draw_work(R, m->cfg.vocab) : 0;
 }
 
 tadm_status tadm_sample_rows(tadm_model* m, const float* logits_dev, int64_t ld, int32_t R, const tadm_row_settings* set,
@@ -2161,7 +2161,7 @@ tadm_status tadm_sample_rows(tadm_model* m, const float* logits_dev, int64_t ld,
   OnDevice dev(m->device);
   HIPCHK(dev.err);
   HIPCHK(draw_rows(DrawRows{logits_dev, (size_t)ld, R, m->cfg.vocab, a.temperature_dev, a.top_k_dev, a.top_p_dev,
-                            a.min_p_dev, u_dev, token_dev, logp_dev}, m->stream));
+                            a.min_p_dev, u_dev, token_dev, logp_dev}, work_dev, m->stream));
   return TADM_OK;
 }
 
