@@ -199,13 +199,23 @@ __device__ __forceinline__ void choose_bin(const H* hist, u64 mark, Shared& s) {
 }
 
 // A row of logits, or a block's share [first, end) of one; first is a multiple of CELL NW.  A wave has every NW-th
-// cell: its lane l the quads at 256 i + 4 l, i < 4.
+// cell: its lane l the quads at 256 i + 4 l, i < 4.  The next cell's are on their way while one is worked on.
 struct Row {
   const float* lg;
   int V;
   float inv;
   int first, end;
+  f32x4 head[4];  // the quads of the wave's first cell, on their way since start()
 
+  __device__ __forceinline__ int first_cell() const { return first / CELL + (int)(threadIdx.x >> 6); }
+  __device__ __forceinline__ void load_cell(int c, f32x4 (&a)[4]) const {
+    const int v = c * CELL + 4 * (threadIdx.x & 63);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) a[i] = load(v + 256 * i);
+  }
+  __device__ __forceinline__ void start() {
+    if (first_cell() * CELL < end) load_cell(first_cell(), head);
+  }
   __device__ __forceinline__ f32x4 load(int v) const {
     f32x4 a;
     if (v + 3 < V) {
@@ -225,15 +235,15 @@ struct Row {
   // f(cell, the lane's first entry, l' of its quads) for the wave's cells
   template <class F>
   __device__ __forceinline__ void cells(F f) const {
-    const int lane = threadIdx.x & 63;
-    for (int c = first / CELL + (threadIdx.x >> 6); c * CELL < end; c += NW) {
-      const int v = c * CELL + 4 * lane;
+    f32x4 next[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) next[i] = head[i];
+    for (int c = first_cell(); c * CELL < end; c += NW) {
       f32x4 a[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) a[i] = load(v + 256 * i);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) a[i] = scaled(a[i]);
-      f(c, v, a);
+      for (int i = 0; i < 4; ++i) a[i] = scaled(next[i]);
+      if ((c + NW) * CELL < end) load_cell(c + NW, next);
+      f(c, c * CELL + 4 * (int)(threadIdx.x & 63), a);
     }
   }
   // f(quad of the cell, the lane's first entry, its four l'), and at a cell's end done(cell)
@@ -507,13 +517,14 @@ __device__ __forceinline__ void weigh_cells(const Row& row, float m, const Cut& 
 
 // A row whose list overflowed, by digits: for the cut of K and that of P, the bins of the entries that the digits
 // chosen so far have left, until these fit a list.
-__device__ __noinline__ Cut cut_by_digits(const Settings& set, const Row& row, float m, Shared& s) {
+__device__ __noinline__ Cut cut_by_digits(Settings set, const float* lg, int V, float m, Shared& s) {
   const int tid = threadIdx.x;
-  Cut cut{-INFINITY, row.V};
+  Row row{lg, V, set.inv, 0, V, {}};
+  Cut cut{-INFINITY, V};
 #pragma unroll 1
   for (int step = 0; step < 2; ++step) {
     const bool count = step == 0;
-    if (count ? set.k >= row.V : set.p == 1u << 24) continue;
+    if (count ? set.k >= V : set.p == 1u << 24) continue;
     u64 mark = set.k;
     int level = 0;
     for (;; ++level) {
@@ -526,6 +537,7 @@ __device__ __noinline__ Cut cut_by_digits(const Settings& set, const Row& row, f
         return (u64)own_exp_term(y);
       };
       clear(s.mass, BINS);
+      row.start();
       __syncthreads();
       row.each([&](float x, int v) {
         const u64 q = weight(x, v, level);
@@ -581,23 +593,14 @@ __device__ __forceinline__ void gather_bins(const Row& row, float m, const Marks
   double sum = 0.0;
   row.quads([&](int i, int v, const f32x4& a) {
     if (i == 0) sum = 0.0;
-    bool listed = false;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const float y = below(a[e], m);
       const float q = own_exp_term(y);
       const uint32_t bin = y > Y_MIN ? (uint32_t)bin_of(y) : BINS;
       sum += bin < k.sure && q >= set.q_min ? (double)q : 0.0;
-      listed |= bin < BINS && k.listed(bin);
+      if (bin < BINS && k.listed(bin) && q > 0.f) put(a[e], v + e, (u64)q);
     }
-    if (listed)
-#pragma unroll 1
-      for (int e = 0; e < 4; ++e) {
-        const float x = e == 0 ? a[0] : e == 1 ? a[1] : e == 2 ? a[2] : a[3], y = below(x, m);
-        if (!(y > Y_MIN) || !k.listed((uint32_t)bin_of(y))) continue;
-        const u64 q = (u64)own_exp_term(y);
-        if (q) put(x, v + e, q);
-      }
   }, [&](int c) {
     const double q = wave_whole(sum);
     if ((threadIdx.x & 63) == 0) cell(c, q);
@@ -646,7 +649,8 @@ __global__ __launch_bounds__(T, 4) void draw_kernel(DrawRows d) {
   __shared__ Shared s;
   const int r = blockIdx.x, tid = threadIdx.x;
   const Settings set = settings_of(d, r);
-  const Row row{d.logits + (size_t)r * d.ld, d.V, set.inv, 0, d.V};
+  Row row{d.logits + (size_t)r * d.ld, d.V, set.inv, 0, d.V, {}};
+  row.start();
   float own = -INFINITY;
   row.cells([&](int, int, const f32x4 (&a)[4]) {
 #pragma unroll
@@ -690,7 +694,7 @@ __global__ __launch_bounds__(T, 4) void draw_kernel(DrawRows d) {
   }
   __syncthreads();
   if (s.n > LIST) {
-    cut = cut_by_digits(set, row, m, s);
+    cut = cut_by_digits(set, row.lg, d.V, m, s);
     weigh_cells(row, m, cut, set, cell);
   } else if (kind != ALL) {
     cut = cut_of(set, kind, k, m, d.V, s);
@@ -720,7 +724,9 @@ struct Split {
 };
 __device__ __forceinline__ Row share_of_row(const Split& a, float inv) {
   const int first = blockIdx.x * a.share;
-  return Row{a.d.logits + (size_t)blockIdx.y * a.d.ld, a.d.V, inv, first, min(first + a.share, a.d.V)};
+  Row row{a.d.logits + (size_t)blockIdx.y * a.d.ld, a.d.V, inv, first, min(first + a.share, a.d.V), {}};
+  row.start();
+  return row;
 }
 // The row's maximum, from those of its parts; own: the thread's.
 struct OwnParts {
@@ -775,10 +781,11 @@ __global__ __launch_bounds__(T, 4) void bins_kernel(Split a) {
   __shared__ Shared s;
   Work& w = a.work[blockIdx.y];
   const Settings set = settings_of(a.d, blockIdx.y);
+  const Row row = share_of_row(a, set.inv);
   OwnParts own;
   const float m = row_max(a, w, s, own);
   if (kind_split(a, set, m) != BY_BINS) return;
-  fill_bins(share_of_row(a, set.inv), m, set, s);
+  fill_bins(row, m, set, s);
   for (int i = threadIdx.x; i < BINS; i += T) {
     if (s.count[i]) atomicAdd(&w.count[i], s.count[i]);
     if (s.mass[i]) atomicAdd(&w.mass[i], s.mass[i]);
@@ -791,12 +798,12 @@ __global__ __launch_bounds__(T, 4) void gather_kernel(Split a) {
   const int tid = threadIdx.x;
   Work& w = a.work[blockIdx.y];
   const Settings set = settings_of(a.d, blockIdx.y);
+  const Row row = share_of_row(a, set.inv);
   OwnParts own;
   const float m = row_max(a, w, s, own);
   if (blockIdx.x == 0 && tid == 0) w.m = m;
   const Kind kind = kind_split(a, set, m);
   if (kind == NOTHING) return;
-  const Row row = share_of_row(a, set.inv);
   if (kind == FIRST) {
     int first = a.d.V;
     row.each([&](float x, int v) {
@@ -856,12 +863,13 @@ __global__ __launch_bounds__(T, 4) void finish_kernel(Split a) {
   const Kind kind = kind_split(a, set, m);
   if (kind == NOTHING) return answer(d, r, -1, -INFINITY);
   if (kind == FIRST) return answer(d, r, first, 0.f);
-  const Row row{d.logits + (size_t)r * d.ld, d.V, set.inv, 0, d.V};
+  Row row{d.logits + (size_t)r * d.ld, d.V, set.inv, 0, d.V, {}};
   const uint32_t n = kind == ALL ? 0 : listed;
   Cut cut{-INFINITY, d.V};
   if (n > LIST) {
-    cut = cut_by_digits(set, row, m, s);
+    cut = cut_by_digits(set, row.lg, d.V, m, s);
     clear(s.cell, CELLS);
+    row.start();
     __syncthreads();
     weigh_cells(row, m, cut, set, [&](int c, double q) { s.cell[c] = (u64)q; });
   } else {
