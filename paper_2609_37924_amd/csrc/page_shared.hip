@@ -27,21 +27,21 @@ struct Item {
   int h, ct, width;    // K/V head, tile of columns
   int t0, t1;          // key tiles: pages, behind the last of them the window's
   int len, np, n;      // positions on pages and their tiles; the row's window (0 on shared pages)
-  int part;            // where its columns' parts begin, -1: it writes the result
-  int pad;
+  int part;            // the first of its units' parts, -1: it writes the result
+  int teams;           // K/V heads h, h + 1, ... that the block's waves share out (few columns, short rows)
 };
 // What a row's columns are joined from: the group's items with h and ct 0, then the row's own.
 struct RowParts {
   int lead, columns;      // first row of the group, columns of its set; no shared part: lead is the row
-  int shared, at_shared;  // splits of the shared pages, and the part of their first item
+  int shared, at_shared;  // splits of the shared pages, and the part of their first unit
   int own, at_own;        // splits of its own keys, ...; own < 0: one, which has written the result
   int pad[2];
 };
-constexpr int PLAN_HEAD = 64;  // bytes before the rows; the first word is the number of items
+constexpr int PLAN_HEAD = 64;  // bytes before the rows; the first words are the number of items and the columns of a row's own
 
 // Sizes of a plan and of what its items write, from what the host knows.
 struct Bounds {
-  int own_width, own_tiles;   // columns of a block on a row's own keys, tiles of them per head
+  int own_width, own_tiles;   // the most columns of a block on a row's own keys, the most tiles of them per head
   int shared_width;           // the most columns of a block on shared pages
   long own_items, shared_items;
 };
@@ -50,7 +50,7 @@ Bounds bounds_of(DType dt, int B, int H, int Hkv, int L) {
   const int ncol = H / Hkv * L;
   Bounds r;
   r.own_width = width_of(dt, ncol);
-  r.own_tiles = tiles_of(ncol, r.own_width);
+  r.own_tiles = tiles_of(ncol, r.own_width > 64 ? 64 : r.own_width);  // the plan takes 64 or 128 columns
   r.shared_width = width_of(dt, B * ncol < 128 ? B * ncol : 128);
   const long own = (long)B * Hkv * r.own_tiles;
   // groups have two rows or more, and each set at most one tile more than its columns fill
@@ -63,186 +63,273 @@ Bounds bounds_of(DType dt, int B, int H, int Hkv, int L) {
 struct PlanArgs {
   PageRows r;
   DType dt;
-  int Hkv, ncol, min_pages;
+  int Hkv, ncol, dh, min_pages;
   int own_items, shared_items;  // room for
-  int own_width, shared_width;
+  int own_width;
   int32_t* plan;
   int32_t *lead, *pages;  // nullable
 };
 
-constexpr int PLAN_THREADS = PAGE_SHARE_ROWS;  // a thread a row
-
-template <class V>
-__device__ __forceinline__ V plan_sum(V v, int* red) {
-  V* r = reinterpret_cast<V*>(red);
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) r[threadIdx.x >> 6] = v;
-  __syncthreads();
-  v = 0;
-#pragma unroll
-  for (int w = 0; w < PLAN_THREADS / 64; ++w) v += r[w];
-  return v;
+// What a block needs for a tile and for everything around its tiles, in 0.1 us, as measured with every CU at work: the slope
+// and the rest of times over prompts of 1 024 to 8 192 positions (16 rows x 64 tokens, 16/4 heads x 128; 8 x 128, 12 x 64).
+// With few columns a tile's bytes come at a CU's share of HBM, or from an L2 where rows read the same pages.
+struct Cost {
+  float tile, again, item;  // again: of a tile that other rows read too
+  int least;                // tiles of a split at least
+};
+__device__ __forceinline__ Cost cost_of(DType dt, int dh, int width) {
+  if (dt == F32) return Cost{4.f, 4.f, 20.f, 4};
+  if (width > 64) return dh > 64 ? Cost{10.f, 10.f, 110.f, 4} : Cost{5.f, 5.f, 85.f, 4};
+  if (width > 32) return dh > 64 ? Cost{8.9f, 8.9f, 45.f, 4} : Cost{3.5f, 3.5f, 40.f, 4};
+  return dh > 64 ? Cost{8.f, 4.2f, 30.f, 2} : Cost{4.f, 2.1f, 30.f, 4};
 }
-__device__ __forceinline__ int plan_scan(int v, int* red) {  // over the threads before this one
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int sum = v;
+constexpr float JOIN = 40.f;  // of parts, where there are any
+// Splits of a unit's tiles that a budget of time for a block's tiles asks for.
+__device__ __forceinline__ int splits_of(int tiles, const Cost& c, float budget) {
+  return max(1, min((int)ceilf(tiles * c.tile / budget), tiles / c.least));
+}
+
+// The threads that plan, one a row: a wave, which needs no barriers, or a block.
+template <int N>
+struct Team {
+  float* red;
+  __device__ __forceinline__ void sync() const {
+    if constexpr (N > 64)
+      __syncthreads();
+    else
+      __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+  }
+  template <bool MAX>
+  __device__ __forceinline__ float over(float v) const {
+    v = MAX ? wave_max(v) : wave_sum(v);
+    if constexpr (N > 64) {
+      __syncthreads();
+      if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+      __syncthreads();
+      v = red[0];
+      for (int w = 1; w < N / 64; ++w) v = MAX ? fmaxf(v, red[w]) : v + red[w];
+    }
+    return v;
+  }
+  __device__ __forceinline__ float sum(float v) const { return over<false>(v); }
+  __device__ __forceinline__ float max(float v) const { return over<true>(v); }
+  // sum over the threads before this one, and over all
+  __device__ __forceinline__ int scan(int v, int& all) const {
+    int upto = v;
 #pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int t = __shfl_up(sum, o, 64);
-    if (lane >= o) sum += t;
+    for (int o = 1; o < 64; o <<= 1) {
+      const int t = __shfl_up(upto, o, 64);
+      if ((int)(threadIdx.x & 63) >= o) upto += t;
+    }
+    all = __builtin_amdgcn_readlane(upto, 63);
+    if constexpr (N > 64) {
+      int* r = reinterpret_cast<int*>(red);
+      const int wave = threadIdx.x >> 6;
+      __syncthreads();
+      if ((threadIdx.x & 63) == 63) r[wave] = upto;
+      __syncthreads();
+      all = 0;
+      for (int w = 0; w < N / 64; ++w) {
+        if (w < wave) upto += r[w];
+        all += r[w];
+      }
+    }
+    return upto - v;
+  }
+};
+
+struct PlanRow {  // of a row; of a group in its first row's place
+  int len, n, common, lead, rows, shared, shared_splits, at_shared, own_splits, at_own, at_item;
+};
+
+// One block; ROWS threads (at least the rows) plan.  What it takes, 6 us, is a launch, two loads behind one another and the
+// steps of the plan; a block of 1 024 threads for every number of rows, with a barrier in every step, took 16 to 22.
+template <int ROWS>
+__global__ __launch_bounds__(1024) void plan_kernel(PlanArgs a) {
+  constexpr int THREADS = 1024;
+  __shared__ PlanRow row[ROWS];
+  __shared__ float red[THREADS / 64];
+  __shared__ int s_alive, s_shared_items, s_own_items, s_teams, s_own_width;
+  const int tid = threadIdx.x, B = a.r.B;
+  if (tid < ROWS) {
+    row[tid].len = tid < B ? row_len(a.r, tid) : 0;
+    row[tid].n = tid < B ? row_new(a.r, tid) : 0;
+  }
+  if (tid == 0) s_alive = 0;
+  __syncthreads();
+  // whole pages that each row and the one before it could share, and those that they do: pages [p0, p0 + width) of
+  // all rows at once, until no two share any further
+  int most = 0;
+  if (tid < ROWS) {
+    most = tid > 0 && tid < B ? min(row[tid].len, row[tid - 1].len) / PAGE : 0;
+    row[tid].common = most;
+    if (most) atomicMax(&s_alive, most);
   }
   __syncthreads();
-  if (lane == 63) red[wave] = sum;
-  __syncthreads();
-  int before = 0;
-#pragma unroll
-  for (int w = 0; w < PLAN_THREADS / 64; ++w) before += w < wave ? red[w] : 0;
-  return before + sum - v;
-}
-
-// Key tiles of an item for a budget of q: the least number of equal runs of at most q.
-__device__ __forceinline__ int splits_of(int tiles, int q) { return tiles > 0 ? (tiles + q - 1) / q : 0; }
-
-// One block, a thread a row.
-__global__ __launch_bounds__(PLAN_THREADS) void plan_kernel(PlanArgs a) {
-  __shared__ int red[PLAN_THREADS / 64];
-  __shared__ int s_common[PLAN_THREADS + 1], s_lead[PLAN_THREADS], s_least[PLAN_THREADS], s_rows[PLAN_THREADS];
-  __shared__ int s_at_shared[PLAN_THREADS + 1], s_at_own[PLAN_THREADS + 1], s_alive;
-  const int b = threadIdx.x, B = a.r.B;
-  const bool mine = b < B;
-  const int len = mine ? row_len(a.r, b) : 0, n = mine ? row_new(a.r, b) : 0;
-  // whole pages that the row and the one before it could share, and those that they do
-  s_rows[b] = len / PAGE;
-  __syncthreads();
-  const int most = mine && b > 0 ? min(s_rows[b], s_rows[b - 1]) : 0;
-  s_common[b] = most;
-  if (b == 0) s_alive = 0;
-  __syncthreads();
-  atomicMax(&s_alive, most);
-  __syncthreads();
-  // pages [p0, p0 + step) of every row at once, until no two rows share any further
-  const int step = max(8 * PLAN_THREADS / B, 64);
+  constexpr int AHEAD = 8;
+  int bits = 6;
+  while ((B << (bits + 1)) <= AHEAD * THREADS) ++bits;
   for (int p0 = 0; p0 < s_alive;) {
-    const int width = min(step, s_alive - p0), total = (B - 1) * width;
-    for (int i = b; i < total; i += PLAN_THREADS) {
-      const int row = 1 + i / width, p = p0 + i % width;
-      if (p < s_common[row]) {
-        const int32_t* t = a.r.table + (size_t)row * a.r.max_pages + p;
-        if (t[0] != t[-(long)a.r.max_pages]) atomicMin(&s_common[row], p);
+    for (int i0 = tid; i0 < (B - 1) << bits; i0 += AHEAD * THREADS) {
+      int x[AHEAD], y[AHEAD];
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) {
+        const int i = i0 + u * THREADS, b = 1 + (i >> bits), p = p0 + (i & ((1 << bits) - 1));
+        x[u] = y[u] = 0;
+        if (b < B && p < row[b].common) {
+          const int32_t* t = a.r.table + (size_t)b * a.r.max_pages + p;
+          x[u] = t[0];
+          y[u] = t[-(long)a.r.max_pages];
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) {
+        const int i = i0 + u * THREADS;
+        if (x[u] != y[u]) atomicMin(&row[1 + (i >> bits)].common, p0 + (i & ((1 << bits) - 1)));
       }
     }
     __syncthreads();
-    p0 += width;
-    if (b == 0) s_alive = 0;
+    p0 += 1 << bits;
+    if (tid == 0) s_alive = 0;
     __syncthreads();
-    if (s_common[b] >= p0 && mine && b > 0 && s_common[b] == most) atomicMax(&s_alive, most);
-    __syncthreads();
-  }
-  // groups: runs of rows that share min_pages pages or more with the row before
-  const int common = mine && s_common[b] >= a.min_pages ? s_common[b] : 0;
-  s_lead[b] = common ? 0 : b;
-  s_least[b] = 1 << 30;
-  s_rows[b] = 0;
-  __syncthreads();
-  for (int o = 1; o < PLAN_THREADS; o <<= 1) {  // the last row at or before this one that begins a group
-    const int v = b >= o ? max(s_lead[b], s_lead[b - o]) : s_lead[b];
-    __syncthreads();
-    s_lead[b] = v;
+    if (tid < ROWS && most > p0 && row[tid].common == most) atomicMax(&s_alive, most);
     __syncthreads();
   }
-  const int lead = s_lead[b];
-  if (mine) atomicAdd(&s_rows[lead], 1);
-  if (common) atomicMin(&s_least[lead], common);
-  __syncthreads();
-  const int rows = mine ? s_rows[lead] : 0, shared = rows > 1 ? s_least[lead] : 0;
-  if (mine && a.lead) a.lead[b] = lead;
-  if (mine && a.pages) a.pages[b] = shared;
 
-  // units (K/V head x tile of columns) and their key tiles, of the group (its first row's thread) and of the row
-  const int np = (len + PAGE - 1) / PAGE;
-  const int own_tiles = n > 0 ? np - shared + (n + PAGE - 1) / PAGE : 0;
-  const int own_units = n > 0 ? a.Hkv * tiles_of(a.ncol, a.own_width) : 0;
-  const int set = rows * a.ncol, set_width = width_of(a.dt, set);
-  const int shared_units = mine && lead == b && shared > 0 ? a.Hkv * tiles_of(set, set_width) : 0;
-  // the least budget of tiles an item that makes no more items than run at once, where the units allow that
-  constexpr int LEAST = 4;
-  const int units = plan_sum(own_units + shared_units, red);
-  const float work = plan_sum((float)own_units * own_tiles + (float)shared_units * shared, red);
-  const int longest = [&] {
-    __syncthreads();
-    if (b == 0) s_alive = LEAST;
-    __syncthreads();
-    atomicMax(&s_alive, max(own_tiles, shared_units ? shared : 0));
-    __syncthreads();
-    return s_alive;
-  }();
-  int q = max(LEAST, (int)fminf(ceilf(work / CHIP), 0x1p30f));
-  if (units <= CHIP) {
-    int lo = q, hi = max(q, longest);  // hi is enough
-    while (lo < hi) {
-      const int mid = (lo + hi) / 2;
-      const int items = plan_sum(own_units * splits_of(own_tiles, mid) + shared_units * splits_of(shared, mid), red);
-      if (items <= CHIP)
-        hi = mid;
-      else
-        lo = mid + 1;
+  RowParts* parts = reinterpret_cast<RowParts*>(a.plan + PLAN_HEAD / 4);
+  if (tid < ROWS) {
+    const Team<ROWS> team{red};
+    const int b = tid;
+    const bool mine = b < B;
+    const int len = row[b].len, n = row[b].n;
+    // groups: runs of rows that share min_pages pages or more with the row before
+    const int common = mine && row[b].common >= a.min_pages ? row[b].common : 0;
+    row[b].lead = common ? 0 : b;
+    row[b].shared = 1 << 30;
+    row[b].rows = 0;
+    team.sync();
+    for (int o = 1; o < ROWS && o < B; o <<= 1) {  // the last row at or before this one that begins a group
+      const int v = b >= o ? max(row[b].lead, row[b - o].lead) : row[b].lead;
+      team.sync();
+      row[b].lead = v;
+      team.sync();
     }
-    q = lo;
-  }
-  const int sp = shared_units ? splits_of(shared, q) : 0, so = own_units ? splits_of(own_tiles, q) : 0;
-  const int at_shared = plan_scan(shared_units * sp, red), at_own = plan_scan(own_units * so, red);
-  s_at_shared[b] = at_shared;
-  s_at_own[b] = at_own;
-  s_common[b] = sp;
-  if (b == PLAN_THREADS - 1) {
-    s_at_shared[b + 1] = at_shared + shared_units * sp;
-    s_at_own[b + 1] = at_own + own_units * so;
+    const int lead = row[b].lead;
+    if (mine) atomicAdd(&row[lead].rows, 1);
+    if (common) atomicMin(&row[lead].shared, common);
+    team.sync();
+    const int rows = row[lead].rows, found = mine && rows > 1 ? row[lead].shared : 0;
+    if (mine && a.lead) a.lead[b] = lead;
+    if (mine && a.pages) a.pages[b] = found;
+
+    // Units (K/V head x tile of columns): the row's, and those of its group.  A group's together where that takes less than
+    // its rows apart, which it does not once a row's columns fill the tiles of a block, and all groups if the work of
+    // the whole call gets less by more than a join.
+    const int set = rows * a.ncol, set_width = width_of(a.dt, set);
+    const Cost cs = cost_of(a.dt, a.dh, set_width);
+    const int pages = (len + PAGE - 1) / PAGE, news = (n + PAGE - 1) / PAGE;
+    const int set_units = a.Hkv * tiles_of(set, set_width);
+    int shared = found, shared_units = 0;
+    {
+      const Cost co = cost_of(a.dt, a.dh, a.own_width);
+      const float row_units = a.Hkv * tiles_of(a.ncol, a.own_width);
+      if (set_units * (found * cs.tile + cs.item) >= rows * row_units * found * co.again) shared = 0;
+      shared_units = mine && lead == b && shared ? set_units : 0;
+      const float apart = n > 0 ? row_units * ((pages - shared + news) * co.tile + shared * co.again + co.item) : 0.f;
+      const float together = (n > 0 ? row_units * ((pages - shared + news) * co.tile + co.item) : 0.f) +
+                             shared_units * (shared * cs.tile + cs.item);
+      if (team.sum(together) + CHIP * JOIN > team.sum(apart)) shared = shared_units = 0;
+    }
+    const bool any_shared = team.max((float)shared) > 0.f;
+    const int own = n > 0 ? pages - shared + news : 0;
+    // Columns of a block on a row's own keys (64 or 128 where it has more than 64) and splits: the choice whose estimate is best.
+    // That is the larger of the work's share a CU and of the rounds that the longer items need; the shorter ones fill the
+    // gaps.  No more items than one a CU beside the units are made.
+    int own_width = a.own_width, teams = 1, own_units = 0, so = 0, ss = 0;
+    float best = 0.f;
+    for (int w = a.own_width; w == a.own_width || w == 64; w -= 64) {
+      const Cost co = cost_of(a.dt, a.dh, w);
+      const int ou = n > 0 ? a.Hkv * tiles_of(a.ncol, w) : 0;
+      // few columns and more rows than blocks: the waves of a block share out several heads, so that each has several tiles
+      const float units = team.sum((float)ou);
+      const int tm = a.dt == F32 || w > 32 ? 1 : units >= 4 * CHIP && a.Hkv % 4 == 0 ? 4 : units >= 2 * CHIP && a.Hkv % 2 == 0 ? 2 : 1;
+      const float own_cost = own * co.tile * tm, shared_cost = shared * cs.tile, blocks = (float)(ou / tm);
+      const float longest = fmaxf(team.max(fmaxf(ou ? own_cost : 0.f, shared_units ? shared_cost : 0.f)), 1.f);
+      for (int j = 0; j < 12; ++j) {
+        // 1, 2, 3, 4, 6, 8, 12, ... 64 splits of the longest unit
+        const float some = longest / (j < 2 ? j + 1 : j & 1 ? 1 << (j + 1) / 2 : 3 << (j - 2) / 2);
+        const int o = tm > 1 ? 1 : splits_of(own, co, some), t = splits_of(shared, cs, some);
+        const float more = team.sum((float)ou * (o - 1) + (float)shared_units * (t - 1));
+        if (more > CHIP) break;
+        const float to = own_cost / o + co.item, ts = shared_cost / t + cs.item;
+        const float work = team.sum(blocks * o * to + shared_units * t * ts);
+        const float top = team.max(fmaxf(ou ? to : 0.f, shared_units ? ts : 0.f));
+        const float large = team.sum((to > 0.5f * top ? blocks * o : 0.f) + (ts > 0.5f * top ? shared_units * t : 0.f));
+        const float time = fmaxf(work / CHIP, ceilf(large / CHIP) * top) + (more > 0.f && !any_shared ? JOIN : 0.f);
+        if ((w == a.own_width && j == 0) || time < best) {
+          best = time;
+          own_width = w;
+          teams = tm;
+          own_units = ou;
+          so = ou ? o : 0;
+          ss = shared_units ? t : 0;
+        }
+      }
+      if (w != 128) break;
+    }
+    int n_shared, n_own;
+    const int at_shared = team.scan(shared_units * ss, n_shared), at_own = team.scan(own_units * so, n_own);
+    row[b].shared_splits = ss;
+    row[b].at_shared = at_shared;
+    row[b].own_splits = so;
+    row[b].at_own = at_own;
+    team.sync();
+    row[b].shared = shared;
+    row[b].rows = rows;
+    if (b == 0) {
+      s_shared_items = min(n_shared, a.shared_items);
+      s_own_items = min(n_own, a.own_items) / teams;
+      s_teams = teams;
+      s_own_width = own_width;
+      a.plan[0] = s_shared_items + s_own_items;
+      a.plan[1] = own_width;
+    }
+    if (mine) {
+      const int gs = shared ? row[lead].shared_splits : 0;
+      parts[b] = RowParts{shared ? lead : b, set, gs, row[lead].at_shared, so == 1 && gs == 0 ? -1 : so, at_own, {0, 0}};
+    }
   }
   __syncthreads();
-  const int n_shared = min(s_at_shared[PLAN_THREADS], a.shared_items), n_own = min(s_at_own[PLAN_THREADS], a.own_items);
-  if (b == 0) a.plan[0] = n_shared + n_own;
-  const int group_splits = s_common[lead], group_at = s_at_shared[lead];
-  RowParts* parts = reinterpret_cast<RowParts*>(a.plan + PLAN_HEAD / 4);
-  if (mine)
-    parts[b] = RowParts{group_splits ? lead : b, group_splits ? set : a.ncol, group_splits, group_at,
-                        so == 1 && group_splits == 0 ? -1 : so, at_own, {0, 0}};
-  s_lead[b] = shared;
-  s_least[b] = so;
   // the items: shared pages first, being the longest; in a row or group, tiles of columns last (items of one head
   // and run of keys are a multiple of 8 apart where heads x splits is, and then run on one XCD)
   Item* items = reinterpret_cast<Item*>(parts + B);
-  __syncthreads();
-  for (int i = b; i < n_shared; i += PLAN_THREADS) {
+  const int n_shared = s_shared_items, n_own = s_own_items, teams = s_teams, own_width = s_own_width;
+  auto owner = [&](auto at, int i) {  // the last row whose first unit is at or before i
     int lo = 0, hi = B;
     while (hi - lo > 1) {
       const int mid = (lo + hi) / 2;
-      if (s_at_shared[mid] <= i)
+      if (at(row[mid]) <= i)
         lo = mid;
       else
         hi = mid;
     }
-    const int splits = s_common[lo], tiles = s_lead[lo], x = i - s_at_shared[lo], per = a.Hkv * splits;
-    const int s = x % splits, h = x / splits % a.Hkv;
-    items[i] = Item{lo, s_rows[lo], h, x / per, width_of(a.dt, s_rows[lo] * a.ncol), (int)((long)tiles * s / splits),
-                    (int)((long)tiles * (s + 1) / splits), tiles * PAGE, tiles, 0, i, 0};
+    return lo;
+  };
+  for (int i = tid; i < n_shared; i += THREADS) {
+    const int b = owner([](const PlanRow& r) { return r.at_shared; }, i);
+    const PlanRow& g = row[b];
+    const int splits = g.shared_splits, x = i - g.at_shared, s = x % splits, h = x / splits % a.Hkv, ct = x / splits / a.Hkv;
+    items[i] = Item{b, g.rows, h, ct, width_of(a.dt, g.rows * a.ncol), (int)((long)g.shared * s / splits),
+                    (int)((long)g.shared * (s + 1) / splits), g.shared * PAGE, g.shared, 0, i, 1};
   }
-  for (int i = b; i < n_own; i += PLAN_THREADS) {
-    int lo = 0, hi = B;
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) / 2;
-      if (s_at_own[mid] <= i)
-        lo = mid;
-      else
-        hi = mid;
-    }
-    const int splits = s_least[lo], x = i - s_at_own[lo], per = a.Hkv * splits;
-    const int s = x % splits, h = x / splits % a.Hkv, row_l = row_len(a.r, lo), row_n = row_new(a.r, lo);
-    const int first = s_lead[lo], pages = (row_l + PAGE - 1) / PAGE, tiles = pages - first + (row_n + PAGE - 1) / PAGE;
-    const bool whole = splits == 1 && s_common[lo] == 0 && first == 0;
-    items[n_shared + i] = Item{lo, 1, h, x / per, a.own_width, first + (int)((long)tiles * s / splits),
-                               first + (int)((long)tiles * (s + 1) / splits), row_l, pages, row_n, whole ? -1 : i, 0};
+  for (int j = tid; j < n_own; j += THREADS) {
+    const int i = j * teams, b = owner([](const PlanRow& r) { return r.at_own; }, i);
+    const PlanRow& g = row[b];
+    const int splits = g.own_splits, x = i - g.at_own, s = x % splits, h = x / splits % a.Hkv, ct = x / splits / a.Hkv;
+    const int pages = (g.len + PAGE - 1) / PAGE, tiles = pages - g.shared + (g.n + PAGE - 1) / PAGE;
+    items[n_shared + j] = Item{b, 1, h, ct, own_width, g.shared + (int)((long)tiles * s / splits),
+                               g.shared + (int)((long)tiles * (s + 1) / splits), g.len, pages, g.n,
+                               splits == 1 && g.shared == 0 ? -1 : i, teams};
   }
 }
 
@@ -270,10 +357,12 @@ struct Strip {
   __device__ __forceinline__ float* part_o(const Args& a, int col) const { return po + (size_t)(col - col0) * a.p.dh; }
   __device__ __forceinline__ float* part_ml(const Args&, int col) const { return pml + 2 * (col - col0); }
 };
-__device__ __forceinline__ Strip strip_of(const Args& a, const Item& i, const Parts& p, bool shared) {
-  Strip s{i.b, i.rows, i.h, i.ct, i.n, i.len, i.np, i.t0, a.k ? i.t1 : min(i.t1, i.np), (size_t)i.b * a.p.Hkv + i.h,
+// (parts of a row's own keys are as wide as their items, those of shared pages as the widest of them)
+__device__ __forceinline__ Strip strip_of(const Args& a, const Item& i, const Parts& p, bool shared, int team = 0) {
+  const int h = i.h + team;
+  Strip s{i.b, i.rows, h, i.ct, i.n, i.len, i.np, i.t0, a.k ? i.t1 : min(i.t1, i.np), (size_t)i.b * a.p.Hkv + h,
           nullptr, nullptr, i.ct * i.width};
-  const size_t at = (size_t)i.part * (shared ? p.shared_width : p.own_width);
+  const size_t at = (size_t)(i.part + team) * (shared ? p.shared_width : i.width);
   if (i.part >= 0) {
     s.po = (shared ? p.o_shared : p.o_own) + at * a.p.dh;
     s.pml = (shared ? p.ml_shared : p.ml_own) + at * 2;
@@ -290,12 +379,14 @@ struct SharedArgs {
 
 // The block's item; false for none, and for one that could not have come from a plan of such rows.
 __device__ __forceinline__ bool item_of(const SharedArgs& s, Item& i) {
-  if ((int)blockIdx.x >= s.plan[0]) return false;
+  // both loads on their way at once
+  const int items = s.plan[0];
   i = reinterpret_cast<const Item*>(s.plan + PLAN_HEAD / 4 + (sizeof(RowParts) / 4) * s.a.r.B)[blockIdx.x];
+  if ((int)blockIdx.x >= items) return false;
   const PageRows& r = s.a.r;
-  const bool row = i.b >= 0 && i.rows >= 1 && i.rows <= r.B && i.b <= r.B - i.rows && (unsigned)i.h < (unsigned)s.a.p.Hkv;
+  const bool row = i.b >= 0 && i.rows >= 1 && i.rows <= r.B && i.b <= r.B - i.rows && i.h >= 0 && i.teams >= 1 && i.h <= s.a.p.Hkv - i.teams;
   const bool keys = i.n >= 0 && i.n <= r.max_n && i.np >= 0 && i.np <= r.max_pages && i.t0 >= 0 && i.t1 <= i.np + (i.n + PAGE - 1) / PAGE;
-  const bool part = i.part < (i.n ? s.own_items : s.shared_items) && i.width <= (i.n ? s.parts.own_width : s.parts.shared_width);
+  const bool part = i.part <= (i.n ? s.own_items : s.shared_items) - i.teams && i.width <= (i.n ? s.parts.own_width : s.parts.shared_width);
   return row && keys && part && i.ct >= 0 && (i.part >= 0 || i.rows == 1);
 }
 
@@ -316,9 +407,20 @@ __global__ __launch_bounds__(64 * WAVES, 2) void shared_bf16_kernel(SharedArgs s
   static_assert(FEW <= wide_lds<DH>(), "the LDS of a block");
   Item i;
   if (!item_of(s, i)) return;
+  float* const xs = reinterpret_cast<float*>(smem);
+  if (i.teams > 1) {
+    const int waves = WAVES / i.teams, team = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / waves;
+    const Strip x = strip_of(s.a, i, s.parts, false, team);
+    float* const mine = xs + team * waves * (2 + DH / 4) * 64;
+    if (i.width == 16 && waves == 2) return narrow_tiles<DH, 1, 2>(s.a, x, mine);
+    if (i.width == 16 && waves == 4) return narrow_tiles<DH, 1, 4>(s.a, x, mine);
+    if (i.width == 32 && waves == 2) return narrow_tiles<DH, 2, 2>(s.a, x, mine);
+    if (i.width == 32 && waves == 4) return narrow_tiles<DH, 2, 4>(s.a, x, mine);
+    return;
+  }
   const Strip x = strip_of(s.a, i, s.parts, i.n == 0);
-  if (i.width == 16) return narrow_tiles<DH, 1, WAVES>(s.a, x, reinterpret_cast<float*>(smem));
-  if (i.width == 32) return narrow_tiles<DH, 2, WAVES>(s.a, x, reinterpret_cast<float*>(smem));
+  if (i.width == 16) return narrow_tiles<DH, 1, WAVES>(s.a, x, xs);
+  if (i.width == 32) return narrow_tiles<DH, 2, WAVES>(s.a, x, xs);
   if constexpr (WIDE) {
     if (i.width == 64)
       wide_tiles<DH, 1, 4>(s.a, x, smem);
@@ -353,12 +455,15 @@ __global__ __launch_bounds__(256) void shared_join_kernel(SharedArgs s) {
     const int first = p.at_shared + (at / width * Hkv + h) * p.shared;
     if (first < 0 || first > s.shared_items - p.shared) return;
     size_t x = (size_t)first * s.parts.shared_width + at % width;
+#pragma unroll 4
     for (int k = 0; k < p.shared; ++k, x += s.parts.shared_width) add(s.parts.ml_shared + 2 * x, s.parts.o_shared + x * dh + d);
   }
-  const int first = p.at_own + (c / s.parts.own_width * Hkv + h) * p.own;
+  const int own_width = min(max(s.plan[1], 1), s.parts.own_width);
+  const int first = p.at_own + (c / own_width * Hkv + h) * p.own;
   if (first < 0 || first > s.own_items - p.own) return;
-  size_t x = (size_t)first * s.parts.own_width + c % s.parts.own_width;
-  for (int k = 0; k < p.own; ++k, x += s.parts.own_width) add(s.parts.ml_own + 2 * x, s.parts.o_own + x * dh + d);
+  size_t x = (size_t)first * own_width + c % own_width;
+#pragma unroll 4
+  for (int k = 0; k < p.own; ++k, x += own_width) add(s.parts.ml_own + 2 * x, s.parts.o_own + x * dh + d);
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
   T* out = static_cast<T*>(a.o) + (((size_t)b * L + j) * Hkv * a.G + h * a.G + g) * dh;
   if (4 * i < dh) store4(out + 4 * i, r[0] * inv, r[1] * inv, r[2] * inv, r[3] * inv);
@@ -384,12 +489,14 @@ size_t page_shared_work(DType dt, int B, int H, int Hkv, int dh, int L) {
   return (size_t)(w.own_items * w.own_width + w.shared_items * w.shared_width) * (dh + 2) * sizeof(float);
 }
 
-hipError_t page_plan(DType dt, const PageRows& r, int H, int Hkv, int min_pages, int32_t* plan, int32_t* lead,
+hipError_t page_plan(DType dt, const PageRows& r, int H, int Hkv, int dh, int min_pages, int32_t* plan, int32_t* lead,
                      int32_t* pages, hipStream_t s) {
   const Bounds w = bounds_of(dt, r.B, H, Hkv, r.max_n);
-  hipLaunchKernelGGL(plan_kernel, dim3(1), dim3(PLAN_THREADS), 0, s,
-                     PlanArgs{r, dt, Hkv, H / Hkv * r.max_n, min_pages, (int)w.own_items, (int)w.shared_items, w.own_width,
-                              w.shared_width, plan, lead, pages});
+  const PlanArgs a{r, dt, Hkv, H / Hkv * r.max_n, dh, min_pages, (int)w.own_items, (int)w.shared_items, w.own_width, plan, lead, pages};
+  if (r.B <= 64)
+    hipLaunchKernelGGL(plan_kernel<64>, dim3(1), dim3(1024), 0, s, a);
+  else
+    hipLaunchKernelGGL(plan_kernel<PAGE_SHARE_ROWS>, dim3(1), dim3(1024), 0, s, a);
   return hipGetLastError();
 }
 

@@ -381,7 +381,7 @@ __device__ __forceinline__ void window_tile(const Args& a, const X& x, int w, co
 template <int DH, int QS, int NW, class X>
 __device__ __forceinline__ void narrow_tiles(const Args& a, const X& x, float* xs) {
   constexpr int NB = DH / 16;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), grp = lane >> 4,
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % NW, grp = lane >> 4,
             fr = lane & 15;
   const int tp = min(x.t1, x.np), first = x.t0 + wave;
   const int steps = first < tp ? (tp - first + NW - 1) / NW : 0;

@@ -99,7 +99,7 @@ constexpr int PAGE_SHARE_ROWS = 1024;  // rows of a plan: a thread of a block ea
 size_t page_plan_bytes(DType dt, int B, int H, int Hkv, int L);
 size_t page_shared_work(DType dt, int B, int H, int Hkv, int dh, int L);
 size_t page_shared_threads(DType dt, int B, int H, int Hkv, int L);
-hipError_t page_plan(DType dt, const PageRows& r, int H, int Hkv, int min_pages, int32_t* plan, int32_t* lead,
+hipError_t page_plan(DType dt, const PageRows& r, int H, int Hkv, int dh, int min_pages, int32_t* plan, int32_t* lead,
                      int32_t* pages, hipStream_t s);
 hipError_t page_attend_shared(DType dt, const PageAttend& a, const int32_t* plan, hipStream_t s);
 

@@ -652,8 +652,8 @@ static tadm_status run_part(tadm_model* m, int first, int count, float* x, int B
                             const tadm_context* ctx, bool prenormed = false) {
   bool pre = prenormed;
   if (count > 0 && ctx && ctx->pool && ctx->share)
-    HIPCHK(page_plan(m->dt, context_rows(ctx, L), m->cfg.n_heads, m->cfg.n_kv_heads, ctx->share, ctx->plan, nullptr, nullptr,
-                     m->stream));
+    HIPCHK(page_plan(m->dt, context_rows(ctx, L), m->cfg.n_heads, m->cfg.n_kv_heads, m->cfg.head_dim, ctx->share, ctx->plan, nullptr,
+                     nullptr, m->stream));
   for (int li = first; li < first + count; ++li) {
     const float* next_norm = li + 1 < first + count ? m->Wf(m->lay.layers[li + 1].attn_norm) : nullptr;
     bool next_pre = false;
@@ -1517,8 +1517,8 @@ tadm_status tadm_pages_share(tadm_model* m, const tadm_page_rows* rows, int32_t 
   OnDevice dev(m->device);
   HIPCHK(dev.err);
   const tadm_config& c = m->cfg;
-  HIPCHK(page_plan(m->dt, page_rows(rows, n), c.n_heads, c.n_kv_heads, min_pages, plan->data_dev, lead_dev, pages_dev,
-                   m->stream));
+  HIPCHK(page_plan(m->dt, page_rows(rows, n), c.n_heads, c.n_kv_heads, c.head_dim, min_pages, plan->data_dev, lead_dev,
+                   pages_dev, m->stream));
   *plan = tadm_page_plan{plan->data_dev, plan->bytes, rows->B, rows->max_pages, rows->len, n, c.n_heads, c.n_kv_heads, c.dtype};
   return TADM_OK;
 }
