@@ -139,8 +139,44 @@ struct Team {
 };
 
 struct PlanRow {  // of a row; of a group in its first row's place
-  int len, n, common, lead, rows, shared, shared_splits, at_shared, own_splits, at_own, at_item;
+  int len, n, common, lead, rows, set, shared, set_units, own, shared_splits, at_shared, own_splits, at_own;
 };
+
+// A way to cut the work of the rows (one a thread of the team) into items, and its time: the longest's where each has a CU
+// of its own, else the larger of the work's share a CU (and half of a shortest item, which come last) and of the rounds
+// that the longer items need; the shorter ones fill the gaps.
+struct Choice {
+  int width, teams, units, own_splits, shared_splits;
+  float time;
+};
+constexpr int SPLITS = 12;  // 1, 2, 3, 4, 6, 8, 12, ... 64 splits of the longest unit
+template <int N>
+__device__ __forceinline__ Choice choice_of(const Team<N>& team, const PlanArgs& a, const PlanRow& r, int width, int j) {
+  Choice c{width, 1, r.n > 0 ? a.Hkv * tiles_of(a.ncol, width) : 0, 0, 0, 0.f};
+  const Cost co = cost_of(a.dt, a.dh, width), cs = cost_of(a.dt, a.dh, width_of(a.dt, r.set));
+  // few columns and more rows than blocks: the waves of a block share out several heads, so that each has several tiles
+  const float units = team.sum((float)c.units);
+  if (a.dt == BF16 && width <= 32)
+    c.teams = units >= 4 * CHIP && a.Hkv % 4 == 0 ? 4 : units >= 2 * CHIP && a.Hkv % 2 == 0 ? 2 : 1;
+  const float own_cost = r.own * co.tile * c.teams, shared_cost = r.shared * cs.tile, blocks = (float)(c.units / c.teams);
+  const float longest = fmaxf(team.max(fmaxf(c.units ? own_cost : 0.f, r.set_units ? shared_cost : 0.f)), 1.f);
+  const float budget = longest / (j < 2 ? j + 1 : j & 1 ? 1 << (j + 1) / 2 : 3 << (j - 2) / 2);
+  const int o = c.teams > 1 ? 1 : splits_of(r.own, co, budget), s = splits_of(r.shared, cs, budget);
+  const float to = own_cost / o + co.item, ts = shared_cost / s + cs.item;
+  const float more = team.sum((float)c.units * (o - 1) + (float)r.set_units * (s - 1));
+  const float work = team.sum(blocks * o * to + r.set_units * s * ts);
+  const float top = team.max(fmaxf(c.units ? to : 0.f, r.set_units ? ts : 0.f));
+  const float large = team.sum((to > 0.5f * top ? blocks * o : 0.f) + (ts > 0.5f * top ? r.set_units * s : 0.f));
+  const float items = team.sum(blocks * o + r.set_units * s);
+  const float least = -team.max(-fminf(c.units ? to : INFINITY, r.set_units ? ts : INFINITY));
+  const bool joins = team.max(r.set_units || (c.units && o > 1) ? 1.f : 0.f) > 0.f;
+  c.own_splits = c.units ? o : 0;
+  c.shared_splits = r.set_units ? s : 0;
+  // no more items than one a CU beside the units: there is room for no more
+  const float rounds = ceilf(large / CHIP) * top;
+  c.time = more > CHIP ? INFINITY : (items > CHIP ? fmaxf(work / CHIP + 0.5f * least, rounds) : top) + (joins ? JOIN : 0.f);
+  return c;
+}
 
 // One block; ROWS threads (at least the rows) plan.  What it takes, 6 us, is a launch, two loads behind one another and the
 // steps of the plan; a block of 1 024 threads for every number of rows, with a barrier in every step, took 16 to 22.
@@ -168,7 +204,8 @@ __global__ __launch_bounds__(1024) void plan_kernel(PlanArgs a) {
   __syncthreads();
   constexpr int AHEAD = 8;
   int bits = 6;
-  while ((B << (bits + 1)) <= AHEAD * THREADS) ++bits;
+  while ((1 << bits) < s_alive && (B << bits) < 2 * AHEAD * THREADS) ++bits;
+  __syncthreads();
   for (int p0 = 0; p0 < s_alive;) {
     for (int i0 = tid; i0 < (B - 1) << bits; i0 += AHEAD * THREADS) {
       int x[AHEAD], y[AHEAD];
@@ -196,7 +233,6 @@ __global__ __launch_bounds__(1024) void plan_kernel(PlanArgs a) {
     __syncthreads();
   }
 
-  RowParts* parts = reinterpret_cast<RowParts*>(a.plan + PLAN_HEAD / 4);
   if (tid < ROWS) {
     const Team<ROWS> team{red};
     const int b = tid;
@@ -240,43 +276,49 @@ __global__ __launch_bounds__(1024) void plan_kernel(PlanArgs a) {
                              shared_units * (shared * cs.tile + cs.item);
       if (team.sum(together) + CHIP * JOIN > team.sum(apart)) shared = shared_units = 0;
     }
-    const bool any_shared = team.max((float)shared) > 0.f;
-    const int own = n > 0 ? pages - shared + news : 0;
-    // Columns of a block on a row's own keys (64 or 128 where it has more than 64) and splits: the choice whose estimate is best.
-    // That is the larger of the work's share a CU and of the rounds that the longer items need; the shorter ones fill the
-    // gaps.  No more items than one a CU beside the units are made.
-    int own_width = a.own_width, teams = 1, own_units = 0, so = 0, ss = 0;
-    float best = 0.f;
-    for (int w = a.own_width; w == a.own_width || w == 64; w -= 64) {
-      const Cost co = cost_of(a.dt, a.dh, w);
-      const int ou = n > 0 ? a.Hkv * tiles_of(a.ncol, w) : 0;
-      // few columns and more rows than blocks: the waves of a block share out several heads, so that each has several tiles
-      const float units = team.sum((float)ou);
-      const int tm = a.dt == F32 || w > 32 ? 1 : units >= 4 * CHIP && a.Hkv % 4 == 0 ? 4 : units >= 2 * CHIP && a.Hkv % 2 == 0 ? 2 : 1;
-      const float own_cost = own * co.tile * tm, shared_cost = shared * cs.tile, blocks = (float)(ou / tm);
-      const float longest = fmaxf(team.max(fmaxf(ou ? own_cost : 0.f, shared_units ? shared_cost : 0.f)), 1.f);
-      for (int j = 0; j < 12; ++j) {
-        // 1, 2, 3, 4, 6, 8, 12, ... 64 splits of the longest unit
-        const float some = longest / (j < 2 ? j + 1 : j & 1 ? 1 << (j + 1) / 2 : 3 << (j - 2) / 2);
-        const int o = tm > 1 ? 1 : splits_of(own, co, some), t = splits_of(shared, cs, some);
-        const float more = team.sum((float)ou * (o - 1) + (float)shared_units * (t - 1));
-        if (more > CHIP) break;
-        const float to = own_cost / o + co.item, ts = shared_cost / t + cs.item;
-        const float work = team.sum(blocks * o * to + shared_units * t * ts);
-        const float top = team.max(fmaxf(ou ? to : 0.f, shared_units ? ts : 0.f));
-        const float large = team.sum((to > 0.5f * top ? blocks * o : 0.f) + (ts > 0.5f * top ? shared_units * t : 0.f));
-        const float time = fmaxf(work / CHIP, ceilf(large / CHIP) * top) + (more > 0.f && !any_shared ? JOIN : 0.f);
-        if ((w == a.own_width && j == 0) || time < best) {
-          best = time;
-          own_width = w;
-          teams = tm;
-          own_units = ou;
-          so = ou ? o : 0;
-          ss = shared_units ? t : 0;
-        }
+    row[b].own = n > 0 ? pages - shared + news : 0;
+    row[b].set_units = shared_units;
+    team.sync();  // the group's pages and rows have been read
+    row[b].shared = shared;
+    row[b].rows = rows;
+    row[b].set = set;
+  }
+  // Columns of a block on a row's own keys (64 or 128 where it has more than 64) and splits: the choice whose estimate is
+  // best; where a wave holds the rows, a wave for each number of splits.
+  __shared__ float s_time[2][SPLITS];
+  const int widths = a.own_width > 64 ? 2 : 1;
+  if constexpr (ROWS == 64) {
+    __syncthreads();
+    const int j = __builtin_amdgcn_readfirstlane(tid >> 6);
+    if (j < SPLITS)
+      for (int v = 0; v < widths; ++v) {
+        const float time = choice_of(Team<64>{red}, a, row[tid & 63], v ? 64 : a.own_width, j).time;
+        if ((tid & 63) == 0) s_time[v][j] = time;
       }
-      if (w != 128) break;
-    }
+    __syncthreads();
+  } else {
+    for (int v = 0; v < widths; ++v)
+      for (int j = 0; j < SPLITS; ++j) {
+        const float time = choice_of(Team<ROWS>{red}, a, row[tid], v ? 64 : a.own_width, j).time;
+        if (tid == 0) s_time[v][j] = time;
+      }
+    __syncthreads();
+  }
+
+  RowParts* parts = reinterpret_cast<RowParts*>(a.plan + PLAN_HEAD / 4);
+  if (tid < ROWS) {
+    const Team<ROWS> team{red};
+    const int b = tid;
+    const bool mine = b < B;
+    // the first of the best, in every wave: lane i looks at the i-th
+    const int lane = tid & 63, at = lane < widths * SPLITS ? lane : 0;
+    const float time = (&s_time[0][0])[at];
+    const int first = __ffsll((unsigned long long)__builtin_amdgcn_ballot_w64(time == -wave_max(-time))) - 1;
+    const int v = first / SPLITS, j = first % SPLITS;
+    const PlanRow mine_row = row[b];
+    const int lead = mine_row.lead, shared = mine_row.shared, shared_units = mine_row.set_units;
+    const Choice c = choice_of(team, a, mine_row, v ? 64 : a.own_width, j);
+    const int own_width = c.width, teams = c.teams, own_units = c.units, so = c.own_splits, ss = c.shared_splits;
     int n_shared, n_own;
     const int at_shared = team.scan(shared_units * ss, n_shared), at_own = team.scan(own_units * so, n_own);
     row[b].shared_splits = ss;
@@ -284,8 +326,6 @@ __global__ __launch_bounds__(1024) void plan_kernel(PlanArgs a) {
     row[b].own_splits = so;
     row[b].at_own = at_own;
     team.sync();
-    row[b].shared = shared;
-    row[b].rows = rows;
     if (b == 0) {
       s_shared_items = min(n_shared, a.shared_items);
       s_own_items = min(n_own, a.own_items) / teams;
@@ -296,7 +336,7 @@ __global__ __launch_bounds__(1024) void plan_kernel(PlanArgs a) {
     }
     if (mine) {
       const int gs = shared ? row[lead].shared_splits : 0;
-      parts[b] = RowParts{shared ? lead : b, set, gs, row[lead].at_shared, so == 1 && gs == 0 ? -1 : so, at_own, {0, 0}};
+      parts[b] = RowParts{shared ? lead : b, mine_row.set, gs, row[lead].at_shared, so == 1 && gs == 0 ? -1 : so, at_own, {0, 0}};
     }
   }
   __syncthreads();
