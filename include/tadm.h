@@ -284,7 +284,7 @@ tadm_status tadm_pages_copy(tadm_model* m, const tadm_pages* p, const int32_t* s
 enum { TADM_STACK_ROWS = 4096 };
 typedef struct {
   int32_t* id_dev;    /* int32 [size] */
-  int32_t* state_dev; /* int32 [4]: free pages, 0, 0, 0 */
+  int32_t* state_dev; /* int32 [4]: free pages, 0, 0, 0; 8-byte aligned */
   int32_t size;
 } tadm_page_stack;
 /* Gives the rows, in their order, the pages that their new tokens need: of all the pages needed, the k-th is the

@@ -895,7 +895,7 @@ __global__ __launch_bounds__(T, 4) void finish_kernel(Split a) {
 // Entries of a block where a row takes several; 0: one block a row.
 int share_for(int R, int V) {
   constexpr int UNIT = CELL * NW;
-  const int most = (V + UNIT - 1) / UNIT, blocks = 512 / R < most ? 512 / R : most;
+  const int most = (V + UNIT - 1) / UNIT, blocks = 1024 / R < most ? 1024 / R : most;
   if (blocks < 2) return 0;
   return ((V + blocks - 1) / blocks + UNIT - 1) / UNIT * UNIT;
 }

@@ -10,8 +10,8 @@
 namespace tadm {
 namespace {
 
-// state: free pages; between the blocks of a launch, pages taken and blocks done (0 outside of one)
-enum { FREE = 0, TAKEN = 1, DONE = 2 };
+// state: free pages, an unused word, and between the blocks of a launch 64 bits, pages taken above blocks done (0 outside of one)
+enum { FREE = 0, PROGRESS = 2 };
 
 __device__ __forceinline__ int up(int x) { return (x + PAGE - 1) / PAGE; }
 
@@ -72,14 +72,12 @@ __global__ __launch_bounds__(256) void assign_kernel(PageStack st, PageRows r, i
       out[j] = (unsigned)id < (unsigned)st.size ? (int64_t)id * PAGE + p % PAGE : -1;
     }
   }
-  if (tid == 0) {  // the last block, when every other has read the count, sets it
-    if (blockIdx.x == 0 && need) atomicAdd(&st.state[TAKEN], need);
-    __threadfence();
-    if (atomicAdd(&st.state[DONE], 1) == (int)(gridDim.x * gridDim.y) - 1) {
-      __threadfence();
-      const int taken = atomicExch(&st.state[TAKEN], 0);
-      st.state[FREE] = free - taken;
-      st.state[DONE] = 0;
+  if (tid == 0) {  // the last block, when every other has read the count, sets it; what each took rides on the same atomic
+    unsigned long long* progress = reinterpret_cast<unsigned long long*>(st.state + PROGRESS);
+    const unsigned long long mine = (unsigned long long)(blockIdx.x == 0 ? need : 0) << 32 | 1, old = atomicAdd(progress, mine);
+    if ((uint32_t)old == gridDim.x * gridDim.y - 1) {
+      st.state[FREE] = free - (int)((old + mine) >> 32);
+      *progress = 0;
     }
   }
 }

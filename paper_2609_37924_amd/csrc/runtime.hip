@@ -1420,7 +1420,8 @@ static_assert(PAGE_STACK_ROWS == TADM_STACK_ROWS, "rows of a call on a stack");
 static tadm_status check_stack(const tadm_page_stack* st, const tadm_page_rows* rows, int n) {
   if (!st || !st->id_dev || !st->state_dev) return fail(TADM_ERR_INVALID, "null stack of pages");
   if (st->size < 1) return fail(TADM_ERR_INVALID, "a stack of %d pages", st->size);
-  if (!aligned(st->id_dev, 4) || !aligned(st->state_dev, 4)) return fail(TADM_ERR_INVALID, "stack not aligned to 4 bytes");
+  if (!aligned(st->id_dev, 4) || !aligned(st->state_dev, 8))
+    return fail(TADM_ERR_INVALID, "stack not aligned to 4 bytes, or its state not to 8");
   TRY(check_rows(rows));
   if (rows->B > TADM_STACK_ROWS) return fail(TADM_ERR_INVALID, "B=%d outside [1, %d]", rows->B, TADM_STACK_ROWS);
   return check_window_size(rows, n, 0);

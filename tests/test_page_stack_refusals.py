@@ -31,7 +31,7 @@ def call(name, st=(), r=(), n=3, granted=BASE, slots=BASE, m=None):
     (dict(state_dev=None), {}, 3, "null stack"),
     (dict(size=0), {}, 3, "0 pages"),
     (dict(id_dev=BASE + 2), {}, 3, "aligned"),
-    (dict(state_dev=BASE + 1), {}, 3, "aligned"),
+    (dict(state_dev=BASE + 4), {}, 3, "state not to 8"),
     ({}, dict(table_dev=None), 3, "table"),
     ({}, dict(B=0), 3, "B=0"),
     ({}, dict(B=4097), 3, "B=4097"),
