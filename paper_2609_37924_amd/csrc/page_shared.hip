@@ -41,22 +41,23 @@ constexpr int PLAN_HEAD = 64;  // bytes before the rows; the first words are the
 
 // Sizes of a plan and of what its items write, from what the host knows.
 struct Bounds {
-  int own_width, own_tiles;   // the most columns of a block on a row's own keys, the most tiles of them per head
-  int shared_width;           // the most columns of a block on shared pages
+  int own_width, shared_width;      // the most columns of a block on a row's own keys, and on shared pages
   long own_items, shared_items;
+  size_t own_columns, shared_columns;  // columns of their parts
 };
 constexpr int CHIP = 256;  // blocks that run at once: one a CU
 Bounds bounds_of(DType dt, int B, int H, int Hkv, int L) {
   const int ncol = H / Hkv * L;
   Bounds r;
   r.own_width = width_of(dt, ncol);
-  r.own_tiles = tiles_of(ncol, r.own_width > 64 ? 64 : r.own_width);  // the plan takes 64 or 128 columns
   r.shared_width = width_of(dt, B * ncol < 128 ? B * ncol : 128);
-  const long own = (long)B * Hkv * r.own_tiles;
+  // Splits add at most one item a CU.  The plan takes 64 or 128 columns where a row has more than 64.
+  const long rows = (long)B * Hkv;
+  r.own_items = rows * tiles_of(ncol, r.own_width > 64 ? 64 : r.own_width) + CHIP;
+  r.own_columns = (size_t)(rows * tiles_of(ncol, r.own_width) + CHIP) * r.own_width;
   // groups have two rows or more, and each set at most one tile more than its columns fill
-  const long shared = B < 2 ? 0 : (long)Hkv * (tiles_of(B * ncol, dt == F32 ? 16 : 128) + B / 2);
-  r.own_items = own + CHIP;  // splits add at most one item a CU
-  r.shared_items = B < 2 ? 0 : shared + CHIP;
+  r.shared_items = B < 2 ? 0 : (long)Hkv * (tiles_of(B * ncol, dt == F32 ? 16 : 128) + B / 2) + CHIP;
+  r.shared_columns = (size_t)r.shared_items * r.shared_width;
   return r;
 }
 
@@ -376,7 +377,8 @@ __global__ __launch_bounds__(1024) void plan_kernel(PlanArgs a) {
 // Where the parts lie: O of the shared items, (m, l) of them, then those of the rows' own.
 struct Parts {
   float *o_shared, *ml_shared, *o_own, *ml_own;
-  int shared_width, own_width;
+  int shared_width, own_width;  // the most
+  size_t shared_columns, own_columns;
 };
 
 // An item as a block's work.
@@ -414,7 +416,6 @@ struct SharedArgs {
   Args a;
   const int32_t* plan;
   Parts parts;
-  int shared_items, own_items;
 };
 
 // The block's item; false for none, and for one that could not have come from a plan of such rows.
@@ -426,27 +427,23 @@ __device__ __forceinline__ bool item_of(const SharedArgs& s, Item& i) {
   const PageRows& r = s.a.r;
   const bool row = i.b >= 0 && i.rows >= 1 && i.rows <= r.B && i.b <= r.B - i.rows && i.h >= 0 && i.teams >= 1 && i.h <= s.a.p.Hkv - i.teams;
   const bool keys = i.n >= 0 && i.n <= r.max_n && i.np >= 0 && i.np <= r.max_pages && i.t0 >= 0 && i.t1 <= i.np + (i.n + PAGE - 1) / PAGE;
-  const bool part = i.part <= (i.n ? s.own_items : s.shared_items) - i.teams && i.width <= (i.n ? s.parts.own_width : s.parts.shared_width);
-  return row && keys && part && i.ct >= 0 && (i.part >= 0 || i.rows == 1);
+  const bool width = i.width >= 16 && i.width <= (i.n ? s.parts.own_width : s.parts.shared_width);
+  const bool part = i.part < 0 ? i.rows == 1 : (size_t)(i.part + i.teams) * (i.n ? i.width : s.parts.shared_width) <=
+                                                   (i.n ? s.parts.own_columns : s.parts.shared_columns);
+  return row && keys && width && part && i.ct >= 0 && i.teams <= 4;
 }
 
 template <int NB>
 __global__ __launch_bounds__(64 * F32_WAVES) void shared_f32_kernel(SharedArgs s) {
   __shared__ float xs[F32_WAVES * (2 + 4 * NB) * 64];
   Item i;
-  if (!item_of(s, i)) return;
-  f32_tiles<NB>(s.a, strip_of(s.a, i, s.parts, i.n == 0), xs);
+  if (item_of(s, i)) f32_tiles<NB>(s.a, strip_of(s.a, i, s.parts, i.n == 0), xs);
 }
 
 constexpr int WAVES = 8;
 // WIDE: sets of more than 32 columns occur.
 template <int DH, bool WIDE>
-__global__ __launch_bounds__(64 * WAVES, 2) void shared_bf16_kernel(SharedArgs s) {
-  constexpr int FEW = WAVES * (2 + DH / 4) * 64 * 4;
-  __shared__ __attribute__((aligned(16))) char smem[WIDE ? wide_lds<DH>() : FEW];
-  static_assert(FEW <= wide_lds<DH>(), "the LDS of a block");
-  Item i;
-  if (!item_of(s, i)) return;
+__device__ __forceinline__ void work_on(const SharedArgs& s, const Item& i, char* smem) {
   float* const xs = reinterpret_cast<float*>(smem);
   if (i.teams > 1) {
     const int waves = WAVES / i.teams, team = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / waves;
@@ -462,11 +459,17 @@ __global__ __launch_bounds__(64 * WAVES, 2) void shared_bf16_kernel(SharedArgs s
   if (i.width == 16) return narrow_tiles<DH, 1, WAVES>(s.a, x, xs);
   if (i.width == 32) return narrow_tiles<DH, 2, WAVES>(s.a, x, xs);
   if constexpr (WIDE) {
-    if (i.width == 64)
-      wide_tiles<DH, 1, 4>(s.a, x, smem);
-    else
-      wide_tiles<DH, 2, 4>(s.a, x, smem);
+    if (i.width == 64) return wide_tiles<DH, 1, 4>(s.a, x, smem);
+    if (i.width == 128) return wide_tiles<DH, 2, 4>(s.a, x, smem);
   }
+}
+template <int DH, bool WIDE>
+__global__ __launch_bounds__(64 * WAVES, 2) void shared_bf16_kernel(SharedArgs s) {
+  constexpr int FEW = WAVES * (2 + DH / 4) * 64 * 4;
+  __shared__ __attribute__((aligned(16))) char smem[WIDE ? wide_lds<DH>() : FEW];
+  static_assert(FEW <= wide_lds<DH>(), "the LDS of a block");
+  Item i;
+  if (item_of(s, i)) work_on<DH, WIDE>(s, i, smem);
 }
 
 // Joins the parts of a column: 32 lanes, four values of the head width each.
@@ -493,14 +496,14 @@ __global__ __launch_bounds__(256) void shared_join_kernel(SharedArgs s) {
   if (p.shared > 0) {
     const int at = (b - p.lead) * ncol + c, width = width_of(sizeof(T) == 2 ? BF16 : F32, p.columns);
     const int first = p.at_shared + (at / width * Hkv + h) * p.shared;
-    if (first < 0 || first > s.shared_items - p.shared) return;
+    if (first < 0 || (size_t)(first + p.shared) * s.parts.shared_width > s.parts.shared_columns) return;
     size_t x = (size_t)first * s.parts.shared_width + at % width;
 #pragma unroll 4
     for (int k = 0; k < p.shared; ++k, x += s.parts.shared_width) add(s.parts.ml_shared + 2 * x, s.parts.o_shared + x * dh + d);
   }
-  const int own_width = min(max(s.plan[1], 1), s.parts.own_width);
+  const int own_width = min(max(s.plan[1], 16), s.parts.own_width);
   const int first = p.at_own + (c / own_width * Hkv + h) * p.own;
-  if (first < 0 || first > s.own_items - p.own) return;
+  if (first < 0 || (size_t)(first + p.own) * own_width > s.parts.own_columns) return;
   size_t x = (size_t)first * own_width + c % own_width;
 #pragma unroll 4
   for (int k = 0; k < p.own; ++k, x += own_width) add(s.parts.ml_own + 2 * x, s.parts.o_own + x * dh + d);
@@ -526,7 +529,7 @@ size_t page_shared_threads(DType dt, int B, int H, int Hkv, int L) {
 
 size_t page_shared_work(DType dt, int B, int H, int Hkv, int dh, int L) {
   const Bounds w = bounds_of(dt, B, H, Hkv, L);
-  return (size_t)(w.own_items * w.own_width + w.shared_items * w.shared_width) * (dh + 2) * sizeof(float);
+  return (w.own_columns + w.shared_columns) * (dh + 2) * sizeof(float);
 }
 
 hipError_t page_plan(DType dt, const PageRows& r, int H, int Hkv, int dh, int min_pages, int32_t* plan, int32_t* lead,
@@ -544,11 +547,10 @@ hipError_t page_attend_shared(DType dt, const PageAttend& c, const int32_t* plan
   const int dh = c.p.dh, G = c.H / c.p.Hkv;
   const Bounds w = bounds_of(dt, c.r.B, c.H, c.p.Hkv, c.r.max_n);
   float* work = static_cast<float*>(c.work);
-  const size_t shared = (size_t)w.shared_items * w.shared_width, own = (size_t)w.own_items * w.own_width;
+  const size_t shared = w.shared_columns, own = w.own_columns;
   SharedArgs a{Args{c.p, c.r, c.q, c.k, c.vt, c.o, c.lse, nullptr, G, c.cap, 1, 1.4426950408889634f / sqrtf((float)dh)}, plan,
                Parts{work, work + (shared + own) * dh, work + shared * dh, work + (shared + own) * dh + 2 * shared, w.shared_width,
-                     w.own_width},
-               (int)w.shared_items, (int)w.own_items};
+                     w.own_width, shared, own}};
   const dim3 grid((unsigned)(w.own_items + w.shared_items));
   if (dt == BF16) {
     const bool wide = c.r.B * G * c.r.max_n > 32;

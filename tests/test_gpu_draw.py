@@ -196,3 +196,28 @@ def test_captured_draws_read_their_settings_at_each_replay():
         eager = torch.zeros_like(token)
         tadm.tadm_sample_rows(m, logits, settings, u, eager, None, work)
         assert torch.equal(eager, token)
+
+
+@pytest.mark.parametrize("V", [700, 5000, 9001])
+def test_more_rows_than_split(V):
+    """A block a row: ordinary rows and rows whose entries hardly differ, which overflow the list."""
+    rng = np.random.default_rng(V)
+    R = 530
+    rows = (rng.normal(size=(R, V)) * rng.uniform(0.02, 4.0, size=(R, 1))).astype(F)
+    for i, kind in enumerate(FLAT):
+        rows[i::40] = FLAT[kind](rng, V)
+    rows[11::40] = -INF
+    check(rows, rng.random(R), mixed(rng, R), V + 2)
+
+
+def test_scratch_is_asked_for():
+    m = model(50304)
+    logits, u, token = torch.zeros(4, 50304, device="cuda"), torch.zeros(4, device="cuda"), torch.zeros(4, dtype=torch.int32, device="cuda")
+    size = tadm.tadm_sample_rows_work(m, 4)
+    assert size > 0 and tadm.tadm_sample_rows_work(m, 0) == 0
+    for work in (None, torch.zeros(size - 16, dtype=torch.uint8, device="cuda"), torch.zeros(size + 16, dtype=torch.uint8, device="cuda")[8:]):
+        with pytest.raises(tadm.TadmError, match="scratch"):
+            tadm.tadm_sample_rows(m, logits, None, u, token, None, work)
+    with pytest.raises(tadm.TadmError, match="apart"):
+        tadm.tadm_sample_rows(m, logits[:, :100].contiguous(), None, u, token, None, torch.zeros(size, dtype=torch.uint8, device="cuda"))
+    assert tadm.tadm_sample_rows_work(m, 5000) == 0  # a block a row needs none
