@@ -88,21 +88,24 @@ struct Cut {
   __device__ __forceinline__ bool has(float xv, int v_) const { return xv > x || (xv == x && v_ <= v); }
 };
 
-struct Shared {
+struct BinsShared {
   u64 mass[BINS];
   uint32_t count[BINS];
+  u64 wave[NW];
+  float wave_f[NW];
+  u64 through;  // the weight of a prefix
+  u64 before;   // what comes before the chosen bin: entries or weight
+  uint32_t bin, n;  // the chosen bin; entries in the list
+};
+struct Shared : BinsShared {
+  u64 sub[BINS];  // bins of the list
   float list_x[LIST];
   int list_v[LIST];
   u64 list_q[LIST];
-  u64 sub[BINS];  // bins of the list
   uint16_t few[LIST];
   u64 cell[CELLS];
-  u64 wave[NW];
-  float wave_f[NW];
   Cut cut;
-  u64 through;         // the weight of a prefix
-  u64 before;          // what comes before the chosen bin: entries or weight
-  uint32_t bin, n, n_few;  // the chosen bin; entries in the list, and of those the few that a cut is among
+  uint32_t n_few;           // of the list, the few that a cut is among
   uint32_t prefix[LEVELS];  // digits chosen so far
   int token;
   u64 rest;
@@ -115,8 +118,21 @@ struct Shared {
     }
   }
 };
+// Of a block that lists entries for another: three blocks a CU.
+struct ListShared : BinsShared {
+  float list_x[LIST];
+  int list_v[LIST];
+  uint32_t at;
+  __device__ __forceinline__ void put(float x, int v) {
+    const uint32_t i = atomicAdd(&n, 1u);
+    if (i < LIST) {
+      list_x[i] = x;
+      list_v[i] = v;
+    }
+  }
+};
 
-__device__ __forceinline__ float block_max(float v, Shared& s) {
+__device__ __forceinline__ float block_max(float v, BinsShared& s) {
   v = wave_max(v);
   if ((threadIdx.x & 63) == 0) s.wave_f[threadIdx.x >> 6] = v;
   __syncthreads();
@@ -175,7 +191,7 @@ struct Bins {
 
 // The bin at which the running sum over the bins reaches `mark` >= 1 (no more than the sum of all); s.bin and
 // s.before (the sum of the bins before it).  before: the sum of those before the thread's.
-__device__ __forceinline__ void pick_bin(u64 before, const Bins& x, u64 mark, Shared& s) {
+__device__ __forceinline__ void pick_bin(u64 before, const Bins& x, u64 mark, BinsShared& s) {
   __syncthreads();
   if (before < mark && before + x.sum() >= mark) {
     uint32_t bin = BPT * threadIdx.x;
@@ -191,7 +207,7 @@ __device__ __forceinline__ void pick_bin(u64 before, const Bins& x, u64 mark, Sh
   __syncthreads();
 }
 template <class H>
-__device__ __forceinline__ void choose_bin(const H* hist, u64 mark, Shared& s) {
+__device__ __forceinline__ void choose_bin(const H* hist, u64 mark, BinsShared& s) {
   const Bins x(hist);
   u64 all;
   const u64 before = block_scan(x.sum(), s.wave, &all);
@@ -355,7 +371,7 @@ struct Marks {
   __device__ __forceinline__ bool listed(uint32_t bin) const { return (bin >= lo && bin <= hi) || bin == k_bin; }
 };
 // From the bins in s (counts where top_k is on, weights where top_p is).
-__device__ __forceinline__ Marks marks_of(const Settings& set, int V, Shared& s) {
+__device__ __forceinline__ Marks marks_of(const Settings& set, int V, BinsShared& s) {
   const int tid = threadIdx.x;
   Marks r{BINS, BINS, BINS, BINS, 0, 0, 0, 0};
   if (set.k < V) {
@@ -607,7 +623,7 @@ __device__ __forceinline__ void gather_bins(const Row& row, float m, const Marks
   });
 }
 // Adds a block's entries to the bins in s.
-__device__ __forceinline__ void fill_bins(const Row& row, float m, const Settings& set, Shared& s) {
+__device__ __forceinline__ void fill_bins(const Row& row, float m, const Settings& set, BinsShared& s) {
   const bool top_k = set.k < row.V, top_p = set.p < 1u << 24;
   for (int i = threadIdx.x; i < BINS; i += T) {
     s.mass[i] = 0;
@@ -635,7 +651,7 @@ __device__ __forceinline__ void add_list(const Cut& cut, const Settings& set, Sh
   }
 }
 // The bin at which the maxima of parts are as many as k; all bins where they are too few.
-__device__ __forceinline__ uint32_t small_bin(int k, Shared& s) {
+__device__ __forceinline__ uint32_t small_bin(int k, BinsShared& s) {
   const Bins x(s.count);
   u64 all;
   const u64 before = block_scan(x.sum(), s.wave, &all);
@@ -733,7 +749,7 @@ struct OwnParts {
   static constexpr int N = PARTS / T;
   float v[N];
 };
-__device__ __forceinline__ float row_max(const Split& a, const Work& w, Shared& s, OwnParts& own) {
+__device__ __forceinline__ float row_max(const Split& a, const Work& w, BinsShared& s, OwnParts& own) {
   const int parts = (a.d.V + PART - 1) / PART;
   float m = -INFINITY;
 #pragma unroll
@@ -748,7 +764,7 @@ __device__ __forceinline__ float row_max(const Split& a, const Work& w, Shared& 
 __device__ __forceinline__ Kind kind_split(const Split& a, const Settings& set, float m) {
   return kind_of(set, m, a.d.V, min(FEW, a.d.V / PART / 2));
 }
-__device__ __forceinline__ void load_bins(const Work& w, Shared& s) {
+__device__ __forceinline__ void load_bins(const Work& w, BinsShared& s) {
   for (int i = threadIdx.x; i < BINS; i += T) {
     s.mass[i] = w.mass[i];
     s.count[i] = w.count[i];
@@ -778,7 +794,7 @@ __global__ __launch_bounds__(T, 4) void parts_kernel(Split a) {
 }
 
 __global__ __launch_bounds__(T, 4) void bins_kernel(Split a) {
-  __shared__ Shared s;
+  __shared__ BinsShared s;
   Work& w = a.work[blockIdx.y];
   const Settings set = settings_of(a.d, blockIdx.y);
   const Row row = share_of_row(a, set.inv);
@@ -793,8 +809,7 @@ __global__ __launch_bounds__(T, 4) void bins_kernel(Split a) {
 }
 
 __global__ __launch_bounds__(T, 4) void gather_kernel(Split a) {
-  __shared__ Shared s;
-  __shared__ uint32_t at;
+  __shared__ ListShared s;
   const int tid = threadIdx.x;
   Work& w = a.work[blockIdx.y];
   const Settings set = settings_of(a.d, blockIdx.y);
@@ -813,7 +828,7 @@ __global__ __launch_bounds__(T, 4) void gather_kernel(Split a) {
     return;
   }
   if (tid == 0) s.n = 0;
-  const auto put = [&](float x, int v, u64 q) { s.put(x, v, q); };
+  const auto put = [&](float x, int v, u64) { s.put(x, v); };
   const auto cell = [&](int c, double q) { w.cell[c] = q; };
   if (kind == ALL) return weigh_cells(row, m, Cut{-INFINITY, a.d.V}, set, cell);
   if (kind == SMALL_K) {
@@ -831,12 +846,12 @@ __global__ __launch_bounds__(T, 4) void gather_kernel(Split a) {
     gather_bins(row, m, k, set, put, cell);
   }
   __syncthreads();
-  if (tid == 0 && s.n) at = atomicAdd(&w.n, s.n);
+  if (tid == 0 && s.n) s.at = atomicAdd(&w.n, s.n);
   __syncthreads();
   for (int i = tid; i < min((int)s.n, LIST); i += T)
-    if (at + i < LIST) {
-      w.x[at + i] = s.list_x[i];
-      w.v[at + i] = s.list_v[i];
+    if (s.at + i < LIST) {
+      w.x[s.at + i] = s.list_x[i];
+      w.v[s.at + i] = s.list_v[i];
     }
 }
 
