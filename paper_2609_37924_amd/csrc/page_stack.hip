@@ -40,7 +40,8 @@ __device__ __forceinline__ int block_total(int v, int* red) {
 
 constexpr int CHUNK = 2048;  // tokens of a block
 
-// grid (chunks of the window, rows).  Bound by its launch, and for long windows by the bytes of the slots.
+// grid (chunks of the window, rows).  Bound by its launch and the atomic that counts the blocks: 64 rows x 1 token 3.9 us,
+// x 4 096 tokens with their slots (2.1 MB) 5.9; in chunks of 512, four times the blocks, 3 us more.
 __global__ __launch_bounds__(256) void assign_kernel(PageStack st, PageRows r, int32_t* table, int32_t* granted,
                                                      int64_t* slot) {
   __shared__ int red[4];
@@ -107,7 +108,8 @@ __device__ __forceinline__ int scan_before(int v, int* red, int* total) {
 }
 
 // One block: the rows' entries one after the other, PER of them a thread, the present ones packed
-// behind the free pages in that order.  Bound by its launch and the way table -> place in the stack.
+// behind the free pages in that order.  Bound by its launch and the way lengths -> entries -> table -> place in the stack:
+// 64 rows x 1 token 4.2 us, x 4 096 tokens 7.4.
 __global__ __launch_bounds__(RELEASE_THREADS) void release_kernel(PageStack st, PageRows r, int32_t* table) {
   __shared__ int at[PAGE_STACK_ROWS + 1];  // the first of each row's entries among all
   __shared__ int red[RELEASE_THREADS / 64];
