@@ -291,11 +291,11 @@ typedef struct {
  * k-th from the back of the stack.  A row gets all of its pages or none: it is granted if it needs none, or if those needed up
  * to and with it are no more than the free ones (so that behind a row that had to wait only rows that need none are
  * granted); one whose positions pass the table is not.  granted_dev [B] receives n_b or 0, a count that
- * tadm_page_rows takes as n_dev.  slot_dev (int64 [B, n], nullable) receives each granted token's place,
- * page * TADM_PAGE + position % TADM_PAGE, -1 where there is none or the page is absent.  The entries
- * of rows that are not granted, and what lies behind the needed ones, stay as they are; the others are written, though
- * the descriptor's table is const.  Lengths are read on the device, so a captured call serves any; they stay as they are
- * (the caller advances them). */
+ * tadm_page_rows takes as n_dev (of a later call: it may not lie over this one's n_dev or len_dev).  slot_dev
+ * (int64 [B, n], nullable) receives each granted token's place, page * TADM_PAGE + position % TADM_PAGE, -1 where
+ * there is none or the page is absent.  The entries of rows that are not granted, and what lies behind the needed ones,
+ * stay as they are; the others are written, though the descriptor's table is const.  Lengths are read on the device, so a
+ * captured call serves any; they stay as they are (the caller advances them). */
 tadm_status tadm_pages_assign(tadm_model* m, const tadm_page_stack* stack, const tadm_page_rows* rows, int32_t n,
                               int32_t* granted_dev, int64_t* slot_dev);
 /* The reverse: takes back the pages of the rows' last tokens, at positions [len_b, len_b + n_b), len_b being what the row

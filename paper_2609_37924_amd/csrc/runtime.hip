@@ -1597,6 +1597,12 @@ tadm_status tadm_pages_assign(tadm_model* m, const tadm_page_stack* stack, const
   TRY(check_stack(stack, rows, n));
   if (!granted_dev) return fail(TADM_ERR_INVALID, "null granted_dev");
   if (!aligned(granted_dev, 4) || !aligned(slot_dev, 8)) return fail(TADM_ERR_INVALID, "granted_dev or slot_dev not aligned");
+  const uintptr_t g = reinterpret_cast<uintptr_t>(granted_dev), bytes = (uintptr_t)rows->B * 4;
+  for (const int32_t* p : {rows->len_dev, rows->n_dev}) {  // blocks read other rows' lengths while these are written
+    const uintptr_t a = reinterpret_cast<uintptr_t>(p);
+    if (p && g < a + bytes && a < g + bytes)
+      return fail(TADM_ERR_INVALID, "granted_dev lies over %s", p == rows->n_dev ? "n_dev" : "len_dev");
+  }
   if (!m) return fail(TADM_ERR_INVALID, "null model");
   TRY(check_own_table(m, rows, "pages for the rows of a pooled context (tadm_context_append takes them)"));
   OnDevice dev(m->device);

@@ -57,6 +57,17 @@ def test_outputs_of_assign():
     assert tadm.lib.tadm_pages_release(None, None, None, 1) == INV
 
 
+@pytest.mark.parametrize("name", ["n_dev", "len_dev"])
+@pytest.mark.parametrize("by", [-4, 0, 4])
+def test_assign_refuses_to_write_over_its_lengths(name, by):
+    """Blocks read the lengths of the rows before theirs while others write what was granted (B=2: 8 bytes each)."""
+    at = BASE + 64
+    assert call("assign", r={name: at}, granted=at + by) == INV
+    assert "granted_dev" in tadm.last_error() and name in tadm.last_error(), tadm.last_error()
+    for clear in (-8, 8):
+        assert call("assign", r={name: at}, granted=at + clear) == INV and "null model" in tadm.last_error()
+
+
 def test_descriptors_refuse_other_tensors():
     ids, state = torch.zeros(8, dtype=torch.int32), torch.zeros(4, dtype=torch.int32)
     assert tadm.page_stack(ids, state).size == 8
