@@ -348,7 +348,8 @@ tadm_status tadm_context_truncate(tadm_context* ctx, int32_t len);
 /* Passes over a pooled context read what neighbouring rows share (the rows of a fork that come from one row) once
  * for all of them, from min_pages (>= 1) shared pages on; 0: each row by itself, as after creation and in a fork.  The
  * results are the same up to the order of sums.  Allocates scratch; not under graph capture (TADM_ERR_STATE), and
- * passes captured before keep what they were captured with.  TADM_ERR_UNSUPPORTED for more than TADM_SHARE_ROWS rows. */
+ * passes captured before keep what they were captured with.  TADM_ERR_UNSUPPORTED for more than TADM_SHARE_ROWS rows, and where a
+ * window of max_seq tokens would take 2^32 threads in a launch. */
 tadm_status tadm_context_share(tadm_context* ctx, int32_t min_pages);
 /* The rows of a pooled context for the operators above (valid until it is destroyed; len as of now).
  * Behind the context's pages the table has absent ones. */

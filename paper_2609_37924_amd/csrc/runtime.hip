@@ -1834,6 +1834,8 @@ tadm_status tadm_context_share(tadm_context* ctx, int32_t min_pages) {
     const tadm_config& c = m->cfg;
     size_t work = 0, plan = 0;
     for (int n = 1; n <= c.max_seq; ++n) {
+      if (page_shared_threads(m->dt, ctx->B, c.n_heads, c.n_kv_heads, n) >> 32)
+        return fail(TADM_ERR_UNSUPPORTED, "%d rows of %d tokens and %d heads: a launch takes 2^32 threads", ctx->B, n, c.n_heads);
       work = std::max(work, page_shared_work(m->dt, ctx->B, c.n_heads, c.n_kv_heads, c.head_dim, n));
       plan = std::max(plan, page_plan_bytes(m->dt, ctx->B, c.n_heads, c.n_kv_heads, n));
     }

@@ -135,6 +135,23 @@ def test_share_refusals():
         tadm.tadm_context_destroy(x)
 
 
+@pytest.mark.parametrize("rows, says", [(1024, "2.32 threads"), (1025, "B=1025 rows")])
+def test_share_refuses_what_no_launch_takes(rows, says):
+    """1 024 rows x 4 096 tokens x 32 heads x 32 lanes of the join are 2^32; nothing is allocated or run."""
+    cfg = synth.get_config("tiny", dtype="f32", n_heads=32, n_kv_heads=32, head_dim=4, d_model=64, vocab=64)
+    m = tadm.tadm_model_create(tadm.make_config(cfg, max_batch=rows, max_seq=4096))
+    pool = tadm.tadm_pool_create(m, 1)
+    ctx = tadm.tadm_context_create_pooled(m, pool, rows, 64)
+    try:
+        with pytest.raises(tadm.TadmError, match=says):
+            tadm.tadm_context_share(ctx, 1)
+        tadm.tadm_context_share(ctx, 0)
+    finally:
+        tadm.tadm_context_destroy(ctx)
+        tadm.tadm_pool_destroy(pool)
+        tadm.tadm_model_destroy(m)
+
+
 @pytest.mark.parametrize("dtype, H, Hkv, dh", [("f32", 4, 4, 16), ("bf16", 16, 16, 128)])
 def test_a_captured_step_of_samples(dtype, H, Hkv, dh):
     """Each replay takes pages for one to three tokens a row, attends over the prompt's shared pages, the row's own and the new
