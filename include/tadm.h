@@ -433,7 +433,8 @@ tadm_status tadm_sample_noalloc(tadm_model* m, const float* logits_dev, const in
  *     floor(floor(2^24 u) T / 2^24), u_dev[r] in [0, 1) (values outside are cut to it);
  *   logp_dev[r] (nullable): log(q / T) of that token.
  * A temperature of 0 or less takes the first entry of the order, with logp 0.  Entries of +inf are a maximum like any
- * other.  A row of NaN and -inf alone gets -1 and -inf.  work_dev (16-byte aligned, NULL when the size is 0) is scratch of at
+ * other.  A row of NaN and -inf alone gets -1 and -inf, as does one whose l' are all -inf in float32 (finite logits
+ * below -3.4e38 temperature, the rest NaN or -inf).  work_dev (16-byte aligned, NULL when the size is 0) is scratch of at
  * least tadm_sample_rows_work bytes; calls that may overlap, captured ones among them, need scratch of their own. */
 enum { TADM_SAMPLE_ROWS = 1 << 21 }; /* rows of a call at most */
 typedef struct {

@@ -9,7 +9,7 @@
 // The token is the least v at which the running sum of F over v exceeds floor(floor(u 2^24) T 2^-24).
 //
 // K and P are prefixes of the order, so each is one entry, its last (a cut).  Entries fall into 2 048 bins of
-// z = 64 (m - l'), which order as they do.  Where the running count or weight over the bins reaches its mark is the
+// m - l' (bin_of), which order as they do.  Where the running count or weight over the bins reaches its mark is the
 // bin of the cut; what lies in the bins before is kept for sure and summed as it is read, and the entries of
 // the bins that a cut may be in go to a list, which is ranked entry by entry.  For a small top_k the bins of the maxima of
 // disjoint parts of the row do: the k-th of those bounds the k-th entry, and the list has a few more than k entries.

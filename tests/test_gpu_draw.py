@@ -72,6 +72,21 @@ def mixed(rng, R):
                 top_p=rng.choice([1.0, 0.999, 0.9, 0.5, 1e-9], size=R), min_p=rng.choice([0.0, 0.0, 0.01, 0.3], size=R))
 
 
+@pytest.mark.parametrize("V", [1000, 32768])
+@pytest.mark.parametrize("R", [3, 600])
+def test_temperatures_at_the_ends_of_float32(V, R):
+    """l' = l (1 / t) in float32: +-inf where that overflows, and -1 for a row of which nothing finite is left."""
+    rng = np.random.default_rng(V + R)
+    rows = rng.normal(size=(R, V)).astype(F)
+    rows[::3] = -5 - np.abs(rows[::3])  # none but -inf at 1e-38
+    rows[1::3, ::7] += 9  # several +inf at 1e-38
+    tiny = np.where(np.arange(R) % 3 < 2, 1e-38, 1e-30)
+    assert D.draw(rows[0], F(0.5), temperature=tiny[0])[0] == -1 and D.draw(rows[1], F(0.5), temperature=tiny[1])[0] >= 0
+    check(rows, rng.random(R), dict(temperature=tiny))
+    check(rows, rng.random(R), dict(temperature=tiny, top_k=[5] * R, top_p=[0.7] * R))
+    check(rows, rng.random(R), dict(temperature=np.where(tiny < 1e-35, 3e38, np.inf)))
+
+
 @pytest.mark.parametrize("V", [1, 2, 3, 5, 63, 64, 257, 1000, 4097, 16384, 16385, 32768, 32771, 50304, 128256, 262143, 262144])
 def test_rows_with_settings_of_their_own(V):
     rng = np.random.default_rng(V)
