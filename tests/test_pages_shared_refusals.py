@@ -27,18 +27,20 @@ def plan(**kw):
 
 
 @pytest.mark.parametrize("r, p, n, least, lead, says", [
-    (dict(table_dev=None), {}, 3, 1, BASE, "table"),
-    (dict(B=0), {}, 3, 1, BASE, "B=0"),
-    (dict(B=1025), {}, 3, 1, BASE, "B=1025"),
-    (dict(len=257), {}, 3, 1, BASE, "257 positions with 4 pages"),
-    ({}, dict(data_dev=None), 3, 1, BASE, "null plan"),
-    ({}, dict(data_dev=BASE + 8), 3, 1, BASE, "aligned"),
-    ({}, {}, 3, 0, BASE, "min_pages=0"),
-    ({}, {}, 0, 1, BASE, "n=0"),
-    ({}, {}, 3, 1, BASE + 2, "aligned"),
+    (dict(table_dev=None), {}, 3, 1, 0, "table"),
+    (dict(B=0), {}, 3, 1, 0, "B=0"),
+    (dict(B=1025), {}, 3, 1, 0, "B=1025"),
+    (dict(len=257), {}, 3, 1, 0, "257 positions with 4 pages"),
+    ({}, dict(data_dev=None), 3, 1, 0, "null plan"),
+    ({}, dict(data_dev=BASE + 8), 3, 1, 0, "aligned"),
+    ({}, {}, 3, 0, 0, "min_pages=0"),
+    ({}, {}, 0, 1, 0, "n=0"),
+    ({}, {}, 3, 1, 2, "aligned"),
     ({}, {}, 3, 1, None, "null model"),
 ])
 def test_share_names_the_wrong_argument(r, p, n, least, lead, says):
+    """lead: where the outputs begin, from an aligned address."""
+    lead = None if lead is None else BASE + lead
     assert tadm.lib.tadm_pages_share(None, C.byref(rows(**r)), n, least, C.byref(plan(**p)), lead, lead) == INV
     assert says in tadm.last_error(), tadm.last_error()
 
