@@ -266,10 +266,16 @@ def tadm_context_destroy(ctx):
 
 
 # ------------------------------------------------------- paged 8-bit K/V
+def _holding(descriptor, *tensors):
+    """A descriptor has addresses only: with the tensors beside them, these live as long as it does."""
+    descriptor.tensors = tensors
+    return descriptor
+
+
 def page_set(data, scale):
     """Descriptor of pages in the caller's tensors: data uint8 (or float8_e4m3fn)
     [n_pages, n_layers, Hkv, 2, 64 * head_dim], scale float32 [n_pages, n_layers, Hkv, 2],
-    both contiguous and kept alive by the caller."""
+    both contiguous.  Like the descriptors below it holds the tensors."""
     n_pages, n_layers, heads, two, width = data.shape
     if two != 2 or width % PAGE or tuple(scale.shape) != (n_pages, n_layers, heads, 2):
         raise ValueError(f"pages of shape {tuple(data.shape)} with scales of shape {tuple(scale.shape)}")
@@ -277,23 +283,22 @@ def page_set(data, scale):
         raise ValueError(f"pages hold uint8 or float8_e4m3fn codes and float32 scales, not {data.dtype} and {scale.dtype}")
     if not (data.is_contiguous() and scale.is_contiguous()):
         raise ValueError("pages and scales must be contiguous")
-    return tadm_pages(data=ptr(data), scale=ptr(scale), n_pages=n_pages, n_layers=n_layers, n_kv_heads=heads,
-                      head_dim=width // PAGE)
+    return _holding(tadm_pages(data=ptr(data), scale=ptr(scale), n_pages=n_pages, n_layers=n_layers, n_kv_heads=heads,
+                               head_dim=width // PAGE), data, scale)
 
 
 def page_rows(table, length, len_dev=None, n_dev=None):
     """Descriptor of a batch: table int32 [B, max_pages] on the device, length the committed
     positions of every row, or the most of any row when the device tensor len_dev (int32
-    [B]) has each row's; n_dev (int32 [B]) the tokens of each row's window.  The caller
-    keeps the tensors alive."""
+    [B]) has each row's; n_dev (int32 [B]) the tokens of each row's window."""
     if table.dim() != 2:
         raise ValueError(f"a table of shape {tuple(table.shape)}")
     for name, t, shape in (("table", table, tuple(table.shape)), ("len_dev", len_dev, (table.shape[0],)),
                            ("n_dev", n_dev, (table.shape[0],))):
         if t is not None and (str(t.dtype) != "torch.int32" or tuple(t.shape) != shape or not t.is_contiguous()):
             raise ValueError(f"{name} must be contiguous int32 of shape {shape}")
-    return tadm_page_rows(table_dev=ptr(table), len_dev=ptr(len_dev), n_dev=ptr(n_dev), B=table.shape[0],
-                          max_pages=table.shape[1], len=length)
+    return _holding(tadm_page_rows(table_dev=ptr(table), len_dev=ptr(len_dev), n_dev=ptr(n_dev), B=table.shape[0],
+                                   max_pages=table.shape[1], len=length), table, len_dev, n_dev)
 
 
 def tadm_pages_append(m, pages, layer, rows, k, vt, n, cap):
@@ -311,11 +316,10 @@ def tadm_pages_attend_work(m, rows, n):
 
 
 def page_plan(data):
-    """Descriptor of a plan that tadm_pages_share lays out in a device tensor of at least tadm_pages_plan_bytes,
-    kept alive by the caller."""
+    """Descriptor of a plan that tadm_pages_share lays out in a device tensor of at least tadm_pages_plan_bytes."""
     if not data.is_contiguous():
         raise ValueError("a plan must be contiguous")
-    return tadm_page_plan(data_dev=ptr(data), bytes=data.numel() * data.element_size())
+    return _holding(tadm_page_plan(data_dev=ptr(data), bytes=data.numel() * data.element_size()), data)
 
 
 def tadm_pages_plan_bytes(m, rows, n):
@@ -356,11 +360,11 @@ def tadm_pages_copy(m, pages, src, dst):
 
 def page_stack(ids, state):
     """Descriptor of a stack of free pages: ids int32 [pages in all], the free ones first, state int32 [4] with their
-    number and three zeros, both on the device and kept alive by the caller."""
+    number and three zeros, both on the device."""
     for name, t, ok in (("ids", ids, ids.dim() == 1), ("state", state, tuple(state.shape) == (4,))):
         if str(t.dtype) != "torch.int32" or not ok or not t.is_contiguous():
             raise ValueError(f"{name}: {t.dtype} of shape {tuple(t.shape)}, expected contiguous int32")
-    return tadm_page_stack(id_dev=ptr(ids), state_dev=ptr(state), size=ids.shape[0])
+    return _holding(tadm_page_stack(id_dev=ptr(ids), state_dev=ptr(state), size=ids.shape[0]), ids, state)
 
 
 def tadm_pages_assign(m, stack, rows, n, granted, slots=None):
@@ -495,13 +499,13 @@ def tadm_sample_noalloc(m, logits, canvas, B, L, canvas_off, pos0, args, next_ca
 
 def row_settings(temperature=None, top_k=None, top_p=None, min_p=None):
     """Settings of each row of a tadm_sample_rows call: contiguous device tensors [R] (float32, top_k int32), None for
-    a setting that is off.  The caller keeps the tensors alive."""
+    a setting that is off."""
     given = dict(temperature=temperature, top_k=top_k, top_p=top_p, min_p=min_p)
     for name, t in given.items():
         kind = "torch.int32" if name == "top_k" else "torch.float32"
         if t is not None and (str(t.dtype) != kind or t.dim() != 1 or not t.is_contiguous()):
             raise ValueError(f"{name} must be contiguous {kind} with an entry for each row")
-    s = tadm_row_settings(**{name + "_dev": ptr(t) for name, t in given.items()})
+    s = _holding(tadm_row_settings(**{name + "_dev": ptr(t) for name, t in given.items()}), *given.values())
     s.rows = {t.shape[0] for t in given.values() if t is not None}
     return s
 
