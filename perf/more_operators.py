@@ -465,8 +465,7 @@ def _own_attend(state):
     if "pages" not in state:  # descriptors and scratch that a program keeps beside its pages
         state["pages"] = tadm.page_set(state["data"], state["scale"])
         state["rows"] = tadm.page_rows(state["table"], _max_pages(c) * PAGE, state["len"], state["new"])
-        state["plan_data"] = torch.empty(tadm.tadm_pages_plan_bytes(m, state["rows"], n), dtype=torch.uint8, device=dev)
-        state["plan"] = tadm.page_plan(state["plan_data"])
+        state["plan"] = tadm.page_plan(torch.empty(tadm.tadm_pages_plan_bytes(m, state["rows"], n), dtype=torch.uint8, device=dev))
         size = tadm.tadm_pages_attend_shared_work(m, state["rows"], n)
         state["work"] = torch.empty(size, dtype=torch.uint8, device=dev)
         state["views"] = [[state[t][i] for t in ("q", "k", "vt", "o", "lse")] for i in range(c["layers"])]
