@@ -244,7 +244,8 @@ size_t tadm_pages_attend_work(const tadm_model* m, const tadm_page_rows* rows, i
  * windows of n tokens: a pass calls it once, before its layers.  lead_dev and pages_dev ([B], nullable) receive each
  * row's group by its first row and the pages that the group shares (0 in a group of one).  data_dev is 16-byte aligned and
  * holds tadm_pages_plan_bytes; the other fields are set by the call.  A plan is of the tables and lengths as they are when it
- * runs: after a change of either it is to be made again (its values are void then, no access leaves the arrays).
+ * runs: after a change of either it is to be made again.  A captured call sets the fields, and each replay lays out the
+ * plan.  By a plan that is out of date or not laid out yet, calls give void values; no access leaves the arrays.
  * At most TADM_SHARE_ROWS rows. */
 enum { TADM_SHARE_ROWS = 1024 };
 typedef struct {

@@ -16,56 +16,13 @@
 // 64 rows x 1 token over 8 192 shared and up to 512 other positions, 32/16 heads x 128: 218 and 47; 16 rows: 57 and 25; 32
 // rows of four prompts: 109 and 41; 32 rows of two over 4 096, 16 heads x 128: 62 and 29, 12 heads x 64: 24 and 15; 16 x 64 tokens
 // over 4 096, 16/4 heads x 128 (not shared, two splits of 128 columns): 68 and 63; 16 x 16 over 8 192, 32/16 heads: 65 and 69.
+#include "page_plan.h"
 #include "page_tiles.h"
 
 namespace tadm {
 namespace {
 
-// Columns of a block by the columns of a set; 16 in float32.
-__host__ __device__ __forceinline__ int width_of(DType dt, int columns) {
-  return dt == F32 || columns <= 16 ? 16 : columns <= 32 ? 32 : columns <= 64 ? 64 : 128;
-}
-__host__ __device__ __forceinline__ int tiles_of(int columns, int width) { return (columns + width - 1) / width; }
-
-// One item of a plan.
-struct Item {
-  int b, rows;         // the row whose pages are read; rows whose columns are in the set
-  int h, ct, width;    // K/V head, tile of columns
-  int t0, t1;          // key tiles: pages, behind the last of them the window's
-  int len, np, n;      // positions on pages and their tiles; the row's window (0 on shared pages)
-  int part;            // the first of its units' parts, -1: it writes the result
-  int teams;           // K/V heads h, h + 1, ... that the block's waves share out (few columns, short rows)
-};
-// What a row's columns are joined from: the group's items with h and ct 0, then the row's own.
-struct RowParts {
-  int lead, columns;      // first row of the group, columns of its set; no shared part: lead is the row
-  int shared, at_shared;  // splits of the shared pages, and the part of their first unit
-  int own, at_own;        // splits of its own keys, ...; own < 0: one, which has written the result
-  int pad[2];
-};
-constexpr int PLAN_HEAD = 64;  // bytes before the rows; the first words are the number of items and the columns of a row's own
-
-// Sizes of a plan and of what its items write, from what the host knows.
-struct Bounds {
-  int own_width, shared_width;      // the most columns of a block on a row's own keys, and on shared pages
-  long own_items, shared_items;
-  size_t own_columns, shared_columns;  // columns of their parts
-};
-constexpr int CHIP = 256;  // blocks that run at once: one a CU
-Bounds bounds_of(DType dt, int B, int H, int Hkv, int L) {
-  const int ncol = H / Hkv * L;
-  Bounds r;
-  r.own_width = width_of(dt, ncol);
-  r.shared_width = width_of(dt, B * ncol < 128 ? B * ncol : 128);
-  // Splits add at most one item a CU.  The plan takes 64 or 128 columns where a row has more than 64.
-  const long rows = (long)B * Hkv;
-  r.own_items = rows * tiles_of(ncol, r.own_width > 64 ? 64 : r.own_width) + CHIP;
-  r.own_columns = (size_t)(rows * tiles_of(ncol, r.own_width) + CHIP) * r.own_width;
-  // groups have two rows or more, and each set at most one tile more than its columns fill
-  r.shared_items = B < 2 ? 0 : (long)Hkv * (tiles_of(B * ncol, dt == F32 ? 16 : 128) + B / 2) + CHIP;
-  r.shared_columns = (size_t)r.shared_items * r.shared_width;
-  return r;
-}
+static_assert(PLAN_PAGE == PAGE, "positions of a page");
 
 struct PlanArgs {
   PageRows r;
@@ -162,7 +119,7 @@ constexpr int SPLITS = 12;  // 1, 2, 3, 4, 6, 8, 12, ... 64 splits of the longes
 template <int N>
 __device__ __forceinline__ Choice choice_of(const Team<N>& team, const PlanArgs& a, const PlanRow& r, int width, int j) {
   Choice c{width, 1, r.n > 0 ? a.Hkv * tiles_of(a.ncol, width) : 0, 0, 0, 0.f};
-  const Cost co = cost_of(a.dt, a.dh, width), cs = cost_of(a.dt, a.dh, width_of(a.dt, r.set));
+  const Cost co = cost_of(a.dt, a.dh, width), cs = cost_of(a.dt, a.dh, width_of(a.dt == F32, r.set));
   // few columns and more rows than blocks: the waves of a block share out several heads, so that each has several tiles
   const float units = team.sum((float)c.units);
   if (a.dt == BF16 && width <= 32)
@@ -271,7 +228,7 @@ __global__ __launch_bounds__(1024) void plan_kernel(PlanArgs a) {
     // Units (K/V head x tile of columns): the row's, and those of its group.  A group's together where that takes less than
     // its rows apart, which it does not once a row's columns fill the tiles of a block, and all groups if the work of
     // the whole call gets less by more than a join.
-    const int set = rows * a.ncol, set_width = width_of(a.dt, set);
+    const int set = rows * a.ncol, set_width = width_of(a.dt == F32, set);
     const Cost cs = cost_of(a.dt, a.dh, set_width);
     const int pages = (len + PAGE - 1) / PAGE, news = (n + PAGE - 1) / PAGE;
     const int set_units = a.Hkv * tiles_of(set, set_width);
@@ -369,7 +326,7 @@ __global__ __launch_bounds__(1024) void plan_kernel(PlanArgs a) {
     const int b = owner([](const PlanRow& r) { return r.at_shared; }, i);
     const PlanRow& g = row[b];
     const int splits = g.shared_splits, x = i - g.at_shared, s = x % splits, h = x / splits % a.Hkv, ct = x / splits / a.Hkv;
-    items[i] = Item{b, g.rows, h, ct, width_of(a.dt, g.rows * a.ncol), (int)((long)g.shared * s / splits),
+    items[i] = Item{b, g.rows, h, ct, width_of(a.dt == F32, g.rows * a.ncol), (int)((long)g.shared * s / splits),
                     (int)((long)g.shared * (s + 1) / splits), g.shared * PAGE, g.shared, 0, i, 1};
   }
   for (int j = tid; j < n_own; j += THREADS) {
@@ -386,8 +343,6 @@ __global__ __launch_bounds__(1024) void plan_kernel(PlanArgs a) {
 // Where the parts lie: O of the shared items, (m, l) of them, then those of the rows' own.
 struct Parts {
   float *o_shared, *ml_shared, *o_own, *ml_own;
-  int shared_width, own_width;  // the most
-  size_t shared_columns, own_columns;
 };
 
 // An item as a block's work.
@@ -397,8 +352,7 @@ struct Strip {
   float *po, *pml;  // of the columns from the item's first on; null: the result
   int col0;
   __device__ __forceinline__ size_t column(const Args& a, int col) const {
-    const int ncol = a.G * a.r.max_n, c = min(col, rows * ncol - 1);
-    return rows == 1 ? head * ncol + c : ((size_t)(b + c / ncol) * a.p.Hkv + h) * ncol + c % ncol;
+    return column_of(a.G * a.r.max_n, a.p.Hkv, b, rows, h, col);
   }
   __device__ __forceinline__ bool wanted(const Args& a, int col) const {
     const int L = a.r.max_n, ncol = a.G * L;
@@ -408,12 +362,20 @@ struct Strip {
   __device__ __forceinline__ float* part_o(const Args& a, int col) const { return po + (size_t)(col - col0) * a.p.dh; }
   __device__ __forceinline__ float* part_ml(const Args&, int col) const { return pml + 2 * (col - col0); }
 };
+struct SharedArgs {
+  Args a;
+  const int32_t* plan;
+  Parts parts;
+  PlanSizes sizes;
+};
 // (parts of a row's own keys are as wide as their items, those of shared pages as the widest of them)
-__device__ __forceinline__ Strip strip_of(const Args& a, const Item& i, const Parts& p, bool shared, int team = 0) {
+__device__ __forceinline__ Strip strip_of(const SharedArgs& x, const Item& i, bool shared, int team = 0) {
+  const Args& a = x.a;
+  const Parts& p = x.parts;
   const int h = i.h + team;
   Strip s{i.b, i.rows, h, i.ct, i.n, i.len, i.np, i.t0, a.k ? i.t1 : min(i.t1, i.np), (size_t)i.b * a.p.Hkv + h,
           nullptr, nullptr, i.ct * i.width};
-  const size_t at = (size_t)(i.part + team) * (shared ? p.shared_width : i.width);
+  const size_t at = (size_t)(i.part + team) * (shared ? x.sizes.shared_width : i.width);
   if (i.part >= 0) {
     s.po = (shared ? p.o_shared : p.o_own) + at * a.p.dh;
     s.pml = (shared ? p.ml_shared : p.ml_own) + at * 2;
@@ -421,32 +383,20 @@ __device__ __forceinline__ Strip strip_of(const Args& a, const Item& i, const Pa
   return s;
 }
 
-struct SharedArgs {
-  Args a;
-  const int32_t* plan;
-  Parts parts;
-};
-
 // The block's item; false for none, and for one that could not have come from a plan of such rows.
 __device__ __forceinline__ bool item_of(const SharedArgs& s, Item& i) {
   // both loads on their way at once
   const int items = s.plan[0];
   i = reinterpret_cast<const Item*>(s.plan + PLAN_HEAD / 4 + (sizeof(RowParts) / 4) * s.a.r.B)[blockIdx.x];
-  if ((int)blockIdx.x >= items) return false;
-  const PageRows& r = s.a.r;
-  const bool row = i.b >= 0 && i.rows >= 1 && i.rows <= r.B && i.b <= r.B - i.rows && i.h >= 0 && i.teams >= 1 && i.h <= s.a.p.Hkv - i.teams;
-  const bool keys = i.n >= 0 && i.n <= r.max_n && i.np >= 0 && i.np <= r.max_pages && i.t0 >= 0 && i.t1 <= i.np + (i.n + PAGE - 1) / PAGE;
-  const bool width = i.width >= 16 && i.width <= (i.n ? s.parts.own_width : s.parts.shared_width);
-  const bool part = i.part < 0 ? i.rows == 1 : (size_t)(i.part + i.teams) * (i.n ? i.width : s.parts.shared_width) <=
-                                                   (i.n ? s.parts.own_columns : s.parts.shared_columns);
-  return row && keys && width && part && i.ct >= 0 && i.teams <= 4;
+  const bool fits = item_fits(i, s.sizes);
+  return ((int)blockIdx.x < items) & fits;
 }
 
 template <int NB>
 __global__ __launch_bounds__(64 * F32_WAVES) void shared_f32_kernel(SharedArgs s) {
   __shared__ float xs[F32_WAVES * (2 + 4 * NB) * 64];
   Item i;
-  if (item_of(s, i)) f32_tiles<NB>(s.a, strip_of(s.a, i, s.parts, i.n == 0), xs);
+  if (item_of(s, i)) f32_tiles<NB>(s.a, strip_of(s, i, i.n == 0), xs);
 }
 
 constexpr int WAVES = 8;
@@ -460,7 +410,7 @@ __device__ __forceinline__ void work_on(const SharedArgs& s, const Item& i, char
   float* const xs = reinterpret_cast<float*>(smem);
   if (i.teams > 1) {
     const int waves = WAVES / i.teams, team = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / waves;
-    const Strip x = strip_of(s.a, i, s.parts, false, team);
+    const Strip x = strip_of(s, i, false, team);
     float* const mine = xs + team * waves * (2 + DH / 4) * 64;
     if (i.width == 16 && waves == 2) return narrow_tiles<DH, 1, 2>(s.a, x, mine);
     if (i.width == 16 && waves == 4) return narrow_tiles<DH, 1, 4>(s.a, x, mine);
@@ -468,7 +418,7 @@ __device__ __forceinline__ void work_on(const SharedArgs& s, const Item& i, char
     if (i.width == 32 && waves == 4) return narrow_tiles<DH, 2, 4>(s.a, x, mine);
     return;
   }
-  const Strip x = strip_of(s.a, i, s.parts, i.n == 0);
+  const Strip x = strip_of(s, i, i.n == 0);
   if (i.width == 16) return narrow_tiles<DH, 1, WAVES>(s.a, x, xs);
   if (i.width == 32) return narrow_tiles<DH, 2, WAVES>(s.a, x, xs);
   if constexpr (WIDE) {
@@ -496,7 +446,10 @@ __global__ __launch_bounds__(256) void shared_join_kernel(SharedArgs s) {
   const int c = (int)(id % ncol), h = (int)(id / ncol % Hkv), b = (int)(id / ncol / Hkv), g = c / L, j = c % L;
   if (j >= row_new(a.r, b)) return;
   const RowParts p = reinterpret_cast<const RowParts*>(s.plan + PLAN_HEAD / 4)[b];
-  if (p.own < 0) return;  // one item has written the result
+  const int own_width = s.plan[1];
+  size_t shared_at, own_at;
+  const bool shared = shared_parts(p, s.sizes, b, h, c, shared_at), own = own_parts(p, s.sizes, own_width, h, c, own_at);
+  if (!own | (!shared & (p.shared > 0))) return;  // nothing to join: one item has written the result (p.own < 0), or no such plan
   const int d = 4 * i < dh ? 4 * i : 0;
   float m = M_NONE, sum = 0.f, r[4] = {0.f, 0.f, 0.f, 0.f};
   auto add = [&](const float* ml, const float* o) {
@@ -507,20 +460,11 @@ __global__ __launch_bounds__(256) void shared_join_kernel(SharedArgs s) {
     for (int e = 0; e < 4; ++e) r[e] = r[e] * f + v[e] * w;
     m = top;
   };
-  if (p.shared > 0) {
-    const int at = (b - p.lead) * ncol + c, width = width_of(sizeof(T) == 2 ? BF16 : F32, p.columns);
-    const int first = p.at_shared + (at / width * Hkv + h) * p.shared;
-    if (first < 0 || (size_t)(first + p.shared) * s.parts.shared_width > s.parts.shared_columns) return;
-    size_t x = (size_t)first * s.parts.shared_width + at % width;
 #pragma unroll 4
-    for (int k = 0; k < p.shared; ++k, x += s.parts.shared_width) add(s.parts.ml_shared + 2 * x, s.parts.o_shared + x * dh + d);
-  }
-  const int own_width = min(max(s.plan[1], 16), s.parts.own_width);
-  const int first = p.at_own + (c / own_width * Hkv + h) * p.own;
-  if (first < 0 || (size_t)(first + p.own) * own_width > s.parts.own_columns) return;
-  size_t x = (size_t)first * own_width + c % own_width;
+  for (int k = 0; k < p.shared; ++k, shared_at += s.sizes.shared_width)
+    add(s.parts.ml_shared + 2 * shared_at, s.parts.o_shared + shared_at * dh + d);
 #pragma unroll 4
-  for (int k = 0; k < p.own; ++k, x += own_width) add(s.parts.ml_own + 2 * x, s.parts.o_own + x * dh + d);
+  for (int k = 0; k < p.own; ++k, own_at += own_width) add(s.parts.ml_own + 2 * own_at, s.parts.o_own + own_at * dh + d);
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
   T* out = static_cast<T*>(a.o) + (((size_t)b * L + j) * Hkv * a.G + h * a.G + g) * dh;
   if (4 * i < dh) store4(out + 4 * i, r[0] * inv, r[1] * inv, r[2] * inv, r[3] * inv);
@@ -530,25 +474,25 @@ __global__ __launch_bounds__(256) void shared_join_kernel(SharedArgs s) {
 }  // namespace
 
 size_t page_plan_bytes(DType dt, int B, int H, int Hkv, int L) {
-  const Bounds w = bounds_of(dt, B, H, Hkv, L);
+  const Bounds w = bounds_of(dt == F32, B, H, Hkv, L);
   return PLAN_HEAD + (size_t)B * sizeof(RowParts) + (size_t)(w.own_items + w.shared_items) * sizeof(Item);
 }
 
 size_t page_shared_threads(DType dt, int B, int H, int Hkv, int L) {
-  const Bounds w = bounds_of(dt, B, H, Hkv, L);
+  const Bounds w = bounds_of(dt == F32, B, H, Hkv, L);
   const size_t items = (size_t)(w.own_items + w.shared_items) * (dt == BF16 ? 64 * WAVES : 64 * F32_WAVES);
   const size_t join = (size_t)B * H * L * 32 + 256;
   return items > join ? items : join;
 }
 
 size_t page_shared_work(DType dt, int B, int H, int Hkv, int dh, int L) {
-  const Bounds w = bounds_of(dt, B, H, Hkv, L);
+  const Bounds w = bounds_of(dt == F32, B, H, Hkv, L);
   return (w.own_columns + w.shared_columns) * (dh + 2) * sizeof(float);
 }
 
 hipError_t page_plan(DType dt, const PageRows& r, int H, int Hkv, int dh, int min_pages, int32_t* plan, int32_t* lead,
                      int32_t* pages, hipStream_t s) {
-  const Bounds w = bounds_of(dt, r.B, H, Hkv, r.max_n);
+  const Bounds w = bounds_of(dt == F32, r.B, H, Hkv, r.max_n);
   const PlanArgs a{r, dt, Hkv, H / Hkv * r.max_n, dh, min_pages, (int)w.own_items, (int)w.shared_items, w.own_width, plan, lead, pages};
   if (r.B <= 64)
     hipLaunchKernelGGL(plan_kernel<64>, dim3(1), dim3(1024), 0, s, a);
@@ -559,12 +503,12 @@ hipError_t page_plan(DType dt, const PageRows& r, int H, int Hkv, int dh, int mi
 
 hipError_t page_attend_shared(DType dt, const PageAttend& c, const int32_t* plan, hipStream_t s) {
   const int dh = c.p.dh, G = c.H / c.p.Hkv;
-  const Bounds w = bounds_of(dt, c.r.B, c.H, c.p.Hkv, c.r.max_n);
+  const Bounds w = bounds_of(dt == F32, c.r.B, c.H, c.p.Hkv, c.r.max_n);
   float* work = static_cast<float*>(c.work);
   const size_t shared = w.shared_columns, own = w.own_columns;
   SharedArgs a{Args{c.p, c.r, c.q, c.k, c.vt, c.o, c.lse, nullptr, G, c.cap, 1, 1.4426950408889634f / sqrtf((float)dh)}, plan,
-               Parts{work, work + (shared + own) * dh, work + shared * dh, work + (shared + own) * dh + 2 * shared, w.shared_width,
-                     w.own_width, shared, own}};
+               Parts{work, work + (shared + own) * dh, work + shared * dh, work + (shared + own) * dh + 2 * shared},
+               PlanSizes{dt == F32, c.r.B, c.p.Hkv, G * c.r.max_n, c.r.max_n, c.r.max_pages, w.own_width, w.shared_width, own, shared}};
   const dim3 grid((unsigned)(w.own_items + w.shared_items));
   if (dt == BF16) {
     const bool wide = c.r.B * G * c.r.max_n > 32;
