@@ -252,13 +252,14 @@ typedef struct {
   int32_t* data_dev;
   size_t bytes;
   int32_t B, max_pages, len, n, n_heads, n_kv_heads, dtype;
+  const int32_t *table_dev, *len_dev, *n_dev;
 } tadm_page_plan;
 tadm_status tadm_pages_share(tadm_model* m, const tadm_page_rows* rows, int32_t n, int32_t min_pages,
                              tadm_page_plan* plan, int32_t* lead_dev, int32_t* pages_dev);
 /* Bytes of a plan of these rows (B) and n; 0 for invalid arguments. */
 size_t tadm_pages_plan_bytes(const tadm_model* m, const tadm_page_rows* rows, int32_t n);
 /* tadm_pages_attend, with the same arguments and results (sums in another order), as the plan says.  TADM_ERR_STATE for
- * a plan of other rows, another n or other heads.  The scratch, of at least tadm_pages_attend_shared_work bytes, is for one call
+ * a plan of other rows (another table, other arrays of lengths, other sizes), another n or other heads.  The scratch, of at least tadm_pages_attend_shared_work bytes, is for one call
  * at a time, as there; a plan may serve calls that overlap. */
 tadm_status tadm_pages_attend_shared(tadm_model* m, const tadm_pages* p, int32_t layer, const tadm_page_rows* rows,
                                      const tadm_page_plan* plan, const void* q_dev, int32_t n, const void* k_dev,

@@ -67,7 +67,8 @@ class tadm_page_rows(C.Structure):
 
 class tadm_page_plan(C.Structure):
     _fields_ = [("data_dev", C.c_void_p), ("bytes", C.c_size_t)] + [
-        (n, C.c_int32) for n in ("B", "max_pages", "len", "n", "n_heads", "n_kv_heads", "dtype")]
+        (n, C.c_int32) for n in ("B", "max_pages", "len", "n", "n_heads", "n_kv_heads", "dtype")] + [
+        (n, C.c_void_p) for n in ("table_dev", "len_dev", "n_dev")]
 
 
 class tadm_page_stack(C.Structure):

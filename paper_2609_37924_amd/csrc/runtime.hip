@@ -1520,7 +1520,8 @@ tadm_status tadm_pages_share(tadm_model* m, const tadm_page_rows* rows, int32_t 
   const tadm_config& c = m->cfg;
   HIPCHK(page_plan(m->dt, page_rows(rows, n), c.n_heads, c.n_kv_heads, c.head_dim, min_pages, plan->data_dev, lead_dev,
                    pages_dev, m->stream));
-  *plan = tadm_page_plan{plan->data_dev, plan->bytes, rows->B, rows->max_pages, rows->len, n, c.n_heads, c.n_kv_heads, c.dtype};
+  *plan = tadm_page_plan{plan->data_dev, plan->bytes, rows->B, rows->max_pages, rows->len, n, c.n_heads, c.n_kv_heads, c.dtype,
+                         rows->table_dev, rows->len_dev, rows->n_dev};
   return TADM_OK;
 }
 
@@ -1543,6 +1544,8 @@ tadm_status tadm_pages_attend_shared(tadm_model* m, const tadm_pages* p, int32_t
       plan->n_heads != c.n_heads || plan->n_kv_heads != c.n_kv_heads || plan->dtype != c.dtype)
     return fail(TADM_ERR_STATE, "plan of %d rows of up to %d positions and %d tokens, %d heads over %d", plan->B, plan->len,
                 plan->n, plan->n_heads, plan->n_kv_heads);
+  if (plan->table_dev != rows->table_dev || plan->len_dev != rows->len_dev || plan->n_dev != rows->n_dev)
+    return fail(TADM_ERR_STATE, "plan of another table or other arrays of lengths");
   const size_t need = tadm_pages_attend_shared_work(m, rows, n);
   if (!work_dev || work_bytes < need || !aligned(work_dev, 16))
     return fail(TADM_ERR_INVALID, "scratch of %zu bytes, %zu needed, aligned to 16", work_dev ? work_bytes : 0, need);
