@@ -208,6 +208,7 @@ def tadm_weight_info(c, index):
 def tadm_model_create(c):
     m = C.c_void_p()
     check(lib.tadm_model_create(C.byref(c), C.byref(m)))
+    m.vocab = c.vocab  # for checks of shapes
     return m
 
 
@@ -512,8 +513,8 @@ def row_settings(temperature=None, top_k=None, top_p=None, min_p=None):
 
 
 def tadm_sample_rows(m, logits, settings, u, token, logp=None, work=None):
-    """logits: float32 [R, vocab], rows at any stride; settings: row_settings or None; u, logp: float32 [R];
-    token: int32 [R]; work: a device tensor of at least tadm_sample_rows_work bytes (None when that is 0)."""
+    """logits: float32 [R, vocab] (the first vocab columns of wider ones), rows at any stride; settings: row_settings or None;
+    u, logp: float32 [R]; token: int32 [R]; work: a device tensor of at least tadm_sample_rows_work bytes (None when that is 0)."""
     if str(logits.dtype) != "torch.float32" or logits.dim() != 2 or logits.stride(1) != 1:
         raise ValueError(f"logits: {logits.dtype} of shape {tuple(logits.shape)}, expected float32 rows")
     R = logits.shape[0]
@@ -522,7 +523,10 @@ def tadm_sample_rows(m, logits, settings, u, token, logp=None, work=None):
             raise ValueError(f"{name} must be contiguous {kind} of {R} rows")
     if settings is not None and settings.rows - {R}:
         raise ValueError(f"settings of {settings.rows} rows for {R}")
-    check(lib.tadm_sample_rows(m, ptr(logits), logits.stride(0) if R > 1 else max(logits.stride(0), logits.shape[1]), R,
+    ld = logits.stride(0) if R > 1 else max(logits.stride(0), logits.shape[1])
+    if logits.shape[1] < getattr(m, "vocab", 0) <= ld:  # the rows' distance alone does not show that they are too short
+        raise ValueError(f"logits of shape {tuple(logits.shape)} for a vocabulary of {m.vocab}")
+    check(lib.tadm_sample_rows(m, ptr(logits), ld, R,
                                None if settings is None else C.byref(settings), ptr(u), ptr(token), ptr(logp), ptr(work),
                                0 if work is None else work.numel() * work.element_size()))
 

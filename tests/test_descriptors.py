@@ -5,8 +5,8 @@ import weakref
 
 import pytest
 
-tadm = pytest.importorskip("paper_2609_37924_amd")
 torch = pytest.importorskip("torch")
+tadm = pytest.importorskip("paper_2609_37924_amd")
 
 
 def i32(*shape):
