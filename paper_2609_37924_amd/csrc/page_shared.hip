@@ -447,9 +447,12 @@ __global__ __launch_bounds__(256) void shared_join_kernel(SharedArgs s) {
   if (j >= row_new(a.r, b)) return;
   const RowParts p = reinterpret_cast<const RowParts*>(s.plan + PLAN_HEAD / 4)[b];
   const int own_width = s.plan[1];
+  const PlanSizes& z = s.sizes;  // on their way beside the row's words: loaded behind the branch, 2 048 blocks took 7.2 us, not 6.2
+  asm volatile("" ::"s"(own_width), "s"(z.Hkv), "s"(z.own_width), "s"(z.shared_width), "s"(z.own_columns), "s"(z.shared_columns));
+  if (p.own < 0) return;  // one item has written the result
   size_t shared_at, own_at;
   const bool shared = shared_parts(p, s.sizes, b, h, c, shared_at), own = own_parts(p, s.sizes, own_width, h, c, own_at);
-  if (!own | (!shared & (p.shared > 0))) return;  // nothing to join: one item has written the result (p.own < 0), or no such plan
+  if (!own | (!shared & (p.shared > 0))) return;  // parts of no such plan
   const int d = 4 * i < dh ? 4 * i : 0;
   float m = M_NONE, sum = 0.f, r[4] = {0.f, 0.f, 0.f, 0.f};
   auto add = [&](const float* ml, const float* o) {
