@@ -259,8 +259,8 @@ tadm_status tadm_pages_share(tadm_model* m, const tadm_page_rows* rows, int32_t 
 /* Bytes of a plan of these rows (B) and n; 0 for invalid arguments. */
 size_t tadm_pages_plan_bytes(const tadm_model* m, const tadm_page_rows* rows, int32_t n);
 /* tadm_pages_attend, with the same arguments and results (sums in another order), as the plan says.  TADM_ERR_STATE for
- * a plan of other rows (another table, other arrays of lengths, other sizes), another n or other heads.  The scratch, of at least tadm_pages_attend_shared_work bytes, is for one call
- * at a time, as there; a plan may serve calls that overlap. */
+ * a plan of other rows (another table, other arrays of lengths, other sizes), another n or other heads.  The scratch, of
+ * at least tadm_pages_attend_shared_work bytes, is for one call at a time, as there; a plan may serve calls that overlap. */
 tadm_status tadm_pages_attend_shared(tadm_model* m, const tadm_pages* p, int32_t layer, const tadm_page_rows* rows,
                                      const tadm_page_plan* plan, const void* q_dev, int32_t n, const void* k_dev,
                                      const void* vt_dev, int32_t cap, void* o_dev, float* lse_dev, void* work_dev,
@@ -349,9 +349,11 @@ tadm_status tadm_context_fork(const tadm_context* src, const int32_t* rows, int3
 tadm_status tadm_context_truncate(tadm_context* ctx, int32_t len);
 /* Passes over a pooled context read what neighbouring rows share (the rows of a fork that come from one row) once
  * for all of them, from min_pages (>= 1) shared pages on; 0: each row by itself, as after creation and in a fork.  The
- * results are the same up to the order of sums.  Allocates scratch; not under graph capture (TADM_ERR_STATE), and
- * passes captured before keep what they were captured with.  TADM_ERR_UNSUPPORTED for more than TADM_SHARE_ROWS rows, and where a
- * window of max_seq tokens would take 2^32 threads in a launch. */
+ * results are the same up to the order of sums.  Each part of a pass (shared, anchor and denoise layers) makes its plan.
+ * Allocates scratch for windows of up to max_seq tokens, about 8 B n_heads max_seq (head_dim + 2) bytes (4.8 GB for 64 rows
+ * of 16 heads x 128 at a max_seq of 4 480); not under graph capture (TADM_ERR_STATE), and passes captured before keep what
+ * they were captured with.  TADM_ERR_UNSUPPORTED for more than TADM_SHARE_ROWS rows, and where a window of max_seq tokens
+ * would take 2^32 threads in a launch. */
 tadm_status tadm_context_share(tadm_context* ctx, int32_t min_pages);
 /* The rows of a pooled context for the operators above (valid until it is destroyed; len as of now).
  * Behind the context's pages the table has absent ones. */

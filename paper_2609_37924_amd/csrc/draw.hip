@@ -13,7 +13,11 @@
 // bin of the cut; what lies in the bins before is kept for sure and summed as it is read, and the entries of
 // the bins that a cut may be in go to a list, which is ranked entry by entry.  For a small top_k the bins of the maxima of
 // disjoint parts of the row do: the k-th of those bounds the k-th entry, and the list has a few more than k entries.
-// A list that overflows (many equal entries) leaves the row to digits of z, of l' and of v, one after the other.
+// A list that overflows leaves the row to digits of z, of l' and of v, one after the other, and to one block: where many entries are
+// equal, and where a bin of 1 / 192 at a cut has more than 2 048, as in rows that are nearly flat for their width.
+// us with top-p 0.5 and normal l' of deviation 2, then flatter: 1 x 262 144 30, 628 at 0.25, 734 at 0.02, 4 399 all equal;
+// 64 x 128 256 56, 403 at 0.1, 2 320 all equal; 1 024 x 32 768 120, 366 at 0.02, 2 083 all equal.  With top-k too the bins of
+// both cuts are listed, and 262 144 entries overflow from 0.5 on (610).
 //
 // A row takes one block, or where that leaves the chip empty several in four launches: maxima of its parts; bins;
 // sure weights and list; the draw.

@@ -11,11 +11,12 @@
 // blocks of each layer's launch take, their tiles balanced over the chip.  A second launch joins
 // the parts of each column in the order of their keys.
 //
-// Sharing saves bytes, and the tiles of blocks that a row's columns do not fill; where they do, it gains little or (the last
-// figures) loses a little.  us a layer on one MI355X, each row by itself and by a plan:
-// 64 rows x 1 token over 8 192 shared and up to 512 other positions, 32/16 heads x 128: 218 and 47; 16 rows: 57 and 25; 32
-// rows of four prompts: 109 and 41; 32 rows of two over 4 096, 16 heads x 128: 62 and 29, 12 heads x 64: 24 and 15; 16 x 64 tokens
-// over 4 096, 16/4 heads x 128 (not shared, two splits of 128 columns): 68 and 63; 16 x 16 over 8 192, 32/16 heads: 65 and 69.
+// Sharing saves bytes, and the tiles of blocks that a row's columns do not fill; where they do, a plan shares nothing, and what it
+// adds is the join.  us a layer on one MI355X, each row by itself and by a plan:
+// 64 rows x 1 token over 8 192 shared and up to 512 other positions, 32/16 heads x 128: 204 and 46; 16 rows: 55 and 25; 32
+// rows of four prompts: 104 and 41; 32 rows of two over 4 096, 16 heads x 128: 61 and 29, 12 heads x 64: 24 and 15; 16 x 16 over 8 192,
+// 32/16 heads: 64 and 65.  Nothing shared: 8 x 1 over 1 000, 12 heads x 64: 7.7 and 9.8; 16 x 64 over 1 024, 16/4 heads x
+// 128: 25.5 and 28.1, over 4 096 64 and 59 (58 and 56 with pages of each row's own, so no gain of sharing).
 #include "page_plan.h"
 #include "page_tiles.h"
 
@@ -383,9 +384,9 @@ __device__ __forceinline__ Strip strip_of(const SharedArgs& x, const Item& i, bo
   return s;
 }
 
-// The block's item; false for none, and for one that could not have come from a plan of such rows.
+// The block's item; false where there is none, or words by which a block would leave the arrays.
 __device__ __forceinline__ bool item_of(const SharedArgs& s, Item& i) {
-  // both loads on their way at once
+  // every load on its way at once: no branch on the number of items before the item's words are there
   const int items = s.plan[0];
   i = reinterpret_cast<const Item*>(s.plan + PLAN_HEAD / 4 + (sizeof(RowParts) / 4) * s.a.r.B)[blockIdx.x];
   const bool fits = item_fits(i, s.sizes);
@@ -401,7 +402,7 @@ __global__ __launch_bounds__(64 * F32_WAVES) void shared_f32_kernel(SharedArgs s
 
 constexpr int WAVES = 8;
 // An item's work.  Bound by what bounds the tiles: the pages' bytes with few columns, the products and exponentials
-// with many (283 Gflop of 4 rows x 256 tokens over 16 640 positions in 292 us with its join, 0.97 PFLOP/s).  A tile of 128 columns
+// with many (283 Gflop of 4 rows x 256 tokens over 16 640 positions in 278 us with its join, 1.0 PFLOP/s).  A tile of 128 columns
 // takes 1.0 us, what is around an item 11; 64 columns 0.89 and 4.5.  WIDE: sets of more than 32 columns occur.
 // One item a block: blocks that took several in turns spilled registers and took 1.4 to 1.5 times as long.  The grid
 // is the most that there may be; blocks without an item cost nothing that could be measured.
